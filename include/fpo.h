@@ -392,6 +392,121 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A,
                const void* const* B, int32_t dtype_B, double* dot, double* sumsq_A,
                double* sumsq_B, float* cos, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * fpo_orthogonalize - orthogonalises matrices (the direction of a Muon step) by
+ * Newton-Schulz products: X = M / (||M||_F + eps), then `steps` times
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X
+ * (X^T X for a matrix with more rows than columns; the result is the same), O = X.
+ * Every singular value s of X becomes p(s) = a s + b s^3 + c s^5, the singular
+ * vectors stay. The default coefficients (3.4445, -4.7750, 2.0315) take values from
+ * about 0.002 to within 0.68 .. 1.21 in five steps; (1.5, -0.5, 0) converges to the
+ * orthogonal polar factor.
+ *
+ *   n_mats      number of matrices (<= 64); any sizes together, those of equal
+ *               (shorter, longer) side are computed in the same launches
+ *   rows, cols  [host] int64 [n_mats], multiples of 8, rows * cols <= 2^29
+ *   M           [host] n_mats pointers to [rows, cols] (dtype), read only
+ *   O           [host] n_mats pointers to [rows, cols] (dtype), out; not aliasing M
+ * dtype FPO_BF16: bf16 in and out; products of fp16 operands (scaled by powers of
+ * two, more digits than bf16), fp32 accumulation. FPO_F32: float32 in and out,
+ * products to about fp32 precision (pairs of fp16, three products).
+ * A matrix of zeros gives zeros (with eps 0 too). Non-finite entries give a matrix
+ * of unspecified values; the other matrices of the call are not affected. Singular
+ * values below about 1e-6 of the norm (fp32: 1e-7) carry rounding noise, enlarged as
+ * they are (3.4445 times a step).
+ * coef  [host] 3 * steps doubles (a, b, c of each step), NULL: the defaults. They are
+ *       refused (FPO_ERR_ARG) if they let a singular value in [0, 1] grow past 1024
+ *       in any step.
+ * Returns FPO_OK or an fpo_status. */
+typedef struct {
+  int32_t dtype; /* fpo_dtype */
+  int32_t steps; /* 1..32; usually 5 */
+  double eps;    /* >= 0; usually 1e-7 */
+  const double* coef;
+} fpo_ns_desc;
+
+size_t fpo_orthogonalize_workspace(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* rows,
+                                   const int64_t* cols);
+int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* rows, const int64_t* cols,
+                      const void* const* M, void* const* O, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * fpo_muon_update - the Muon step on fp32 masters: momentum, orthogonalisation of
+ * the direction, decoupled weight decay. For each matrix m, with g = s grad (s the
+ * gradient clip's factor, 1 if it is off):
+ *   b' = momentum b + g  (g at step 1; the buffer's content is then ignored)
+ *   u  = g + momentum b' with nesterov, else b'
+ *   O  = fpo_orthogonalize(u)
+ *   W' = (1 - lr weight_decay) W - lr scale O
+ * scale: FPO_MUON_SCALE_NONE 1; _SPECTRAL sqrt(max(1, rows / cols)); _RMS
+ * 0.2 sqrt(max(rows, cols)) (entries of the size AdamW's steps have).
+ * clip_frac, clip_target: as in fpo_opt; FPO_CLIP_UPDATE bounds ||W' - W||_F by
+ * clip_frac ||W||_F (orthogonalising undoes any scaling of the gradient but for its
+ * weight against the momentum).
+ *
+ *   rows, cols  as in fpo_orthogonalize; W, grad, state are [rows, cols]
+ *   grad        [host] n_mats pointers to float gradients
+ *   grad_sumsq  double [n_mats] ||grad||_F^2; required for the gradient clip only
+ *   upd         W_master, state1 (momentum; may be NULL, the array or an entry, if
+ *               momentum is 0), W_lp (dtype desc->ns.dtype), clip_scale as in
+ *               fpo_update_bufs; W_sumsq may be NULL if clip_frac <= 0, else (and
+ *               whenever given) in ||W||_F^2, out ||W'||_F^2; state2 is ignored
+ * ns.dtype sets the precision of the products and the type of W_lp; everything else
+ * is float32.
+ * Returns FPO_OK or an fpo_status. */
+typedef enum { FPO_MUON_SCALE_NONE = 0, FPO_MUON_SCALE_SPECTRAL = 1, FPO_MUON_SCALE_RMS = 2 } fpo_muon_scale;
+typedef struct {
+  fpo_ns_desc ns;
+  double lr, momentum, weight_decay, clip_frac;
+  int64_t step;        /* 1-based */
+  int32_t nesterov;    /* 0 or 1 */
+  int32_t scale;       /* fpo_muon_scale */
+  int32_t clip_target; /* fpo_clip_target */
+} fpo_muon;
+
+size_t fpo_muon_update_workspace(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, const int64_t* cols);
+int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, const int64_t* cols,
+                    const float* const* grad, const double* grad_sumsq, const fpo_update_bufs* upd, void* ws,
+                    size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * fpo_layernorm - layer norm over the last dimension, for models that have it where
+ * others have RMSNorm:
+ *   mu = mean x_t;  sigma = sqrt(mean (x_t - mu)^2 + eps)
+ *   y_t = gain (x_t - mu) / sigma + bias
+ *   x, y        [T, d] (dtype); y must not alias x
+ *   gain, bias  [d] (dtype), each nullable: ones, zeros
+ *   mean, rstd  float [T] out, nullable: mu and 1 / sigma
+ * T <= 2^23, d a multiple of 8, d <= 2^22.
+ * Returns FPO_OK or an fpo_status. */
+typedef struct {
+  int64_t T, d;
+  int32_t dtype;    /* fpo_dtype */
+  int32_t dy_dtype; /* fpo_dtype of dy (fpo_layernorm_vjp) */
+  float eps;
+  float min_std;    /* floor on sigma in the VJP (0: the exact gradient), as min_rms is on rho */
+} fpo_ln_desc;
+
+int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, const void* bias, void* y, float* mean,
+                  float* rstd, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * fpo_layernorm_vjp - the layer norm's VJP, its sigma floored as the RMSNorm VJPs'
+ * rho is (App. E "Min-RMS clamp"), and the gradients of gain and bias (of the forward
+ * pass as it is, whose sigma has no floor). The statistics are computed from x again.
+ *   v = gain dy_t;  sigma~ = max(sigma, min_std);  x^ = (x_t - mu) / sigma~
+ *   dx_t = (v - mean v - x^ mean(v x^)) / sigma~
+ *   dgain = sum_t dy_t (x_t - mu) / sigma,  dbias = sum_t dy_t
+ *   x            [T, d] (dtype);  gain [d] (dtype), nullable: ones
+ *   dy           [T, d] (dy_dtype): e.g. fpo_output_error's g_pre
+ *   dx           float [T, d] out, nullable;  dx_lp [T, d] (dtype) out, nullable: dx rounded once
+ *   dgain, dbias float [d] out, each nullable; sums in a fixed order
+ * At least one output is required.
+ * Returns FPO_OK or an fpo_status. */
+size_t fpo_layernorm_vjp_workspace(const fpo_ln_desc* desc);
+int fpo_layernorm_vjp(const fpo_ln_desc* desc, const void* x, const void* gain, const void* dy, float* dx,
+                      void* dx_lp, float* dgain, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

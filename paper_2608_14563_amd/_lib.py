@@ -16,6 +16,7 @@ FPO_F32, FPO_BF16 = 0, 1
 FPO_MODE_W3, FPO_MODE_FULL_MLP, FPO_MODE_POST_FFN, FPO_MODE_GRAD_BF16, FPO_MODE_PRE_MLP = 0, 1, 2, 4, 8  # bit flags
 FPO_OPT_SGD, FPO_OPT_ADAMW = 0, 1
 FPO_CLIP_GRADIENT, FPO_CLIP_UPDATE = 0, 1
+FPO_MUON_SCALE_NONE, FPO_MUON_SCALE_SPECTRAL, FPO_MUON_SCALE_RMS = 0, 1, 2
 
 STATUS_NAMES = {0: "FPO_OK", 1: "FPO_ERR_NULL", 2: "FPO_ERR_SHAPE", 3: "FPO_ERR_DTYPE", 4: "FPO_ERR_ARG",
                 5: "FPO_ERR_WORKSPACE", 6: "FPO_ERR_UNSUPPORTED", 7: "FPO_ERR_HIP"}
@@ -24,6 +25,8 @@ EXPORTS = (
     "fpo_abi_version", "fpo_last_error", "fpo_output_error_workspace", "fpo_output_error",
     "fpo_pseudograd_workspace", "fpo_pseudograd", "fpo_apply_update_workspace", "fpo_apply_update",
     "fpo_cosine_workspace", "fpo_cosine", "fpo_apply_update_noalloc",
+    "fpo_orthogonalize_workspace", "fpo_orthogonalize", "fpo_muon_update_workspace", "fpo_muon_update",
+    "fpo_layernorm", "fpo_layernorm_vjp_workspace", "fpo_layernorm_vjp",
 )
 NOALLOC_SCRATCH_BYTES = 8 << 20  # FPO_NOALLOC_SCRATCH_BYTES
 
@@ -62,6 +65,21 @@ class PreMlp(C.Structure):
 
 class Overlap(C.Structure):
     _fields_ = [("side_stream", C.c_void_p), ("ready_event", C.c_void_p), ("done_event", C.c_void_p)]
+
+
+class NsDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("steps", C.c_int32), ("eps", C.c_double), ("coef", C.POINTER(C.c_double))]
+
+
+class Muon(C.Structure):
+    _fields_ = [("ns", NsDesc), ("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double),
+                ("clip_frac", C.c_double), ("step", C.c_int64), ("nesterov", C.c_int32), ("scale", C.c_int32),
+                ("clip_target", C.c_int32)]
+
+
+class LnDesc(C.Structure):
+    _fields_ = [("T", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("dy_dtype", C.c_int32),
+                ("eps", C.c_float), ("min_std", C.c_float)]
 
 
 ABI_VERSION = 7
@@ -116,6 +134,22 @@ def load() -> C.CDLL:
     lib.fpo_cosine.restype = C.c_int
     lib.fpo_cosine.argtypes = [C.c_int64, C.POINTER(C.c_int64), PP, PP, C.c_int32, VP, VP, VP, VP, VP,
                                C.c_size_t, VP]
+    PI = C.POINTER(C.c_int64)
+    lib.fpo_orthogonalize_workspace.restype = C.c_size_t
+    lib.fpo_orthogonalize_workspace.argtypes = [C.POINTER(NsDesc), C.c_int64, PI, PI]
+    lib.fpo_orthogonalize.restype = C.c_int
+    lib.fpo_orthogonalize.argtypes = [C.POINTER(NsDesc), C.c_int64, PI, PI, PP, PP, VP, C.c_size_t, VP]
+    lib.fpo_muon_update_workspace.restype = C.c_size_t
+    lib.fpo_muon_update_workspace.argtypes = [C.POINTER(Muon), C.c_int64, PI, PI]
+    lib.fpo_muon_update.restype = C.c_int
+    lib.fpo_muon_update.argtypes = [C.POINTER(Muon), C.c_int64, PI, PI, PP, VP, C.POINTER(UpdateBufs), VP, C.c_size_t,
+                                    VP]
+    lib.fpo_layernorm.restype = C.c_int
+    lib.fpo_layernorm.argtypes = [C.POINTER(LnDesc), VP, VP, VP, VP, VP, VP, VP]
+    lib.fpo_layernorm_vjp_workspace.restype = C.c_size_t
+    lib.fpo_layernorm_vjp_workspace.argtypes = [C.POINTER(LnDesc)]
+    lib.fpo_layernorm_vjp.restype = C.c_int
+    lib.fpo_layernorm_vjp.argtypes = [C.POINTER(LnDesc), VP, VP, VP, VP, VP, VP, VP, VP, C.c_size_t, VP]
     _lib = lib
     return lib
 

@@ -1,5 +1,4 @@
-"""Python binding of libfpo: the four calls of include/fpo.h under the same
-names, taking torch tensors. Argument marshalling only: every step of the
+"""Python binding of libfpo: the calls of include/fpo.h under the same names, taking torch tensors. Argument marshalling only: every step of the
 path runs in the HIP library; torch supplies device memory and the stream.
 
 All tensors must be on the same CUDA (HIP) device and contiguous. The
@@ -19,7 +18,9 @@ from . import _lib as L
 __all__ = [
     "fpo_abi_version", "fpo_output_error", "fpo_output_error_workspace", "fpo_pseudograd", "PostFfn", "PreMlp",
     "fpo_pseudograd_workspace", "fpo_apply_update", "fpo_apply_update_workspace", "fpo_cosine", "Overlap",
-    "fpo_cosine_workspace", "OptConfig", "workspace", "dtype_code",
+    "fpo_cosine_workspace", "OptConfig", "workspace", "dtype_code", "fpo_orthogonalize",
+    "fpo_orthogonalize_workspace", "MuonConfig", "fpo_muon_update", "fpo_muon_update_workspace", "fpo_layernorm",
+    "fpo_layernorm_vjp", "fpo_layernorm_vjp_workspace", "MUON_SCALE_NONE", "MUON_SCALE_SPECTRAL", "MUON_SCALE_RMS",
 ]
 
 
@@ -337,4 +338,146 @@ def fpo_cosine(A, B=None, dot=None, sumsq_A=None, sumsq_B=None, cos=None, ws=Non
                            _p(dot, F64, n, dev, "dot"), _p(sumsq_A, F64, n, dev, "sumsq_A"),
                            _p(sumsq_B, F64, n, dev, "sumsq_B"), _p(cos, F32, n, dev, "cos"),
                            _p(ws, None, None, dev, "ws"), _nbytes(ws), _stream(dev)))
+    return ws
+
+
+# --------------------------------------------------------------------- orthogonalisation, the Muon step
+MUON_SCALE_NONE, MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = (L.FPO_MUON_SCALE_NONE, L.FPO_MUON_SCALE_SPECTRAL,
+                                                        L.FPO_MUON_SCALE_RMS)
+
+
+def _ns_desc(keep: _Keep, dtype: torch.dtype, steps: int, coefs, eps: float) -> L.NsDesc:
+    """coefs: None, one (a, b, c) for every step, or one for each."""
+    c = None
+    if coefs is not None:
+        coefs = [tuple(k) for k in coefs] if len(coefs) and not isinstance(coefs[0], (int, float)) else [tuple(coefs)] * steps
+        if len(coefs) != steps or any(len(k) != 3 for k in coefs):
+            raise ValueError(f"coefs: (a, b, c), or {steps} of them")
+        c = (C.c_double * (3 * steps))(*[float(v) for k in coefs for v in k])
+        keep.refs.append(c)
+    return L.NsDesc(dtype_code(dtype), steps, eps, c)
+
+
+def _sides(keep: _Keep, shapes):
+    for i, s in enumerate(shapes):
+        if len(s) != 2:
+            raise ValueError(f"matrix {i}: shape {tuple(s)}, expected two dimensions")
+    return keep.i64([s[0] for s in shapes]), keep.i64([s[1] for s in shapes])
+
+
+def fpo_orthogonalize_workspace(shapes: Sequence, dtype: torch.dtype) -> int:
+    k = _Keep()
+    desc = _ns_desc(k, dtype, 1, None, 0.0)
+    return L.load().fpo_orthogonalize_workspace(C.byref(desc), len(shapes), *_sides(k, shapes))
+
+
+def fpo_orthogonalize(M, O, steps: int = 5, coefs=None, eps: float = 1e-7, ws=None):
+    """O[i] = the Newton-Schulz orthogonalisation of the matrix M[i] (bfloat16 or
+    float32, all the same); any shapes together. coefs: (a, b, c), or one for
+    each step (default: 3.4445, -4.7750, 2.0315). The workspace does not depend
+    on the steps."""
+    n = len(M)
+    k = _Keep()
+    if n == 0 or len(O) != n:
+        raise ValueError(f"M and O: {n} and {len(O)} matrices")
+    op, dev = M[0].dtype, M[0].device
+    shapes = [tuple(m.shape) for m in M]
+    desc = _ns_desc(k, op, steps, coefs, eps)
+    rows, cols = _sides(k, shapes)
+    lib = L.load()
+    if ws is None:
+        ws = workspace(lib.fpo_orthogonalize_workspace(C.byref(desc), n, rows, cols), dev)
+    L.check(lib.fpo_orthogonalize(C.byref(desc), n, rows, cols, k.arr(M, op, None, dev, n, "M"),
+                                  k.arr(O, op, lambda i: shapes[i], dev, n, "O"), _p(ws, None, None, dev, "ws"),
+                                  _nbytes(ws), _stream(dev)))
+    return ws
+
+
+@dataclass
+class MuonConfig:
+    lr: float = 2e-4
+    momentum: float = 0.95
+    nesterov: bool = True
+    weight_decay: float = 0.01
+    scale: int = L.FPO_MUON_SCALE_RMS  # O is scaled by 0.2 sqrt(max(rows, cols)); or _SPECTRAL, _NONE
+    steps: int = 5
+    coefs: Optional[Sequence] = None
+    eps: float = 1e-7
+    clip_frac: float = 0.01
+    step: int = 1
+    clip_target: int = L.FPO_CLIP_UPDATE  # or FPO_CLIP_GRADIENT: bound the gradient before the momentum
+
+    def c(self, keep: _Keep, dtype: torch.dtype) -> L.Muon:
+        return L.Muon(_ns_desc(keep, dtype, self.steps, self.coefs, self.eps), self.lr, self.momentum,
+                      self.weight_decay, self.clip_frac, self.step, int(self.nesterov), self.scale, self.clip_target)
+
+
+def fpo_muon_update_workspace(shapes: Sequence, dtype: torch.dtype = torch.bfloat16) -> int:
+    k = _Keep()
+    o = MuonConfig().c(k, dtype)
+    return L.load().fpo_muon_update_workspace(C.byref(o), len(shapes), *_sides(k, shapes))
+
+
+def fpo_muon_update(opt: MuonConfig, grad, W_master, state, W_sumsq=None, grad_sumsq=None, W_lp=None, clip_scale=None,
+                    dtype: torch.dtype = torch.bfloat16, ws=None):
+    """The Muon step on float32 masters (matrices of any shapes). state: the
+    momentum buffers (None only with momentum 0). dtype: precision of the
+    products and type of W_lp. W_sumsq (float64, in/out) is needed by the clip
+    (clip_frac > 0), grad_sumsq by the gradient clip only."""
+    n = len(grad)
+    k = _Keep()
+    if n == 0:
+        raise ValueError("grad: no matrices")
+    dev = grad[0].device
+    shapes = [tuple(g.shape) for g in grad]
+    o = opt.c(k, dtype)
+    rows, cols = _sides(k, shapes)
+    lib = L.load()
+    if ws is None:
+        ws = workspace(lib.fpo_muon_update_workspace(C.byref(o), n, rows, cols), dev)
+
+    def shape(i):
+        return shapes[i]
+
+    if W_master is None:
+        raise ValueError("W_master is required")
+    ub = L.UpdateBufs(k.arr(W_master, F32, shape, dev, n, "W_master"), k.arr(W_lp, dtype, shape, dev, n, "W_lp"),
+                      k.arr(state, F32, shape, dev, n, "state"), None, _p(W_sumsq, F64, n, dev, "W_sumsq"),
+                      _p(clip_scale, F32, n, dev, "clip_scale"))
+    L.check(lib.fpo_muon_update(C.byref(o), n, rows, cols, k.arr(grad, F32, None, dev, n, "grad"),
+                                _p(grad_sumsq, F64, n, dev, "grad_sumsq"), C.byref(ub), _p(ws, None, None, dev, "ws"),
+                                _nbytes(ws), _stream(dev)))
+    return ws
+
+
+# --------------------------------------------------------------------- layer norm
+def fpo_layernorm(x, gain, bias, y, mean=None, rstd=None, eps=1e-5):
+    """Layer norm of the rows of x [T, d] into y; gain and bias [d] may be None."""
+    T, d = x.shape
+    op, dev = x.dtype, x.device
+    desc = L.LnDesc(T, d, dtype_code(op), L.FPO_F32, eps, 0.0)
+    L.check(L.load().fpo_layernorm(
+        C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"), _p(bias, op, (d,), dev, "bias"),
+        _p(y, op, (T, d), dev, "y"), _p(mean, F32, (T,), dev, "mean"), _p(rstd, F32, (T,), dev, "rstd"), _stream(dev)))
+
+
+def fpo_layernorm_vjp_workspace(T: int, d: int) -> int:
+    desc = L.LnDesc(T, d, L.FPO_F32, L.FPO_F32, 0.0, 0.0)
+    return L.load().fpo_layernorm_vjp_workspace(C.byref(desc))
+
+
+def fpo_layernorm_vjp(x, gain, dy, dx=None, dx_lp=None, dgain=None, dbias=None, eps=1e-5, min_std=0.0, ws=None):
+    """The layer norm's VJP at x for dy [T, d] (bfloat16 or float32): dx (float32)
+    and dx_lp (x's dtype), with sigma floored at min_std, and the gradients of
+    gain and bias (float32). Any of them may be None."""
+    T, d = x.shape
+    op, dev = x.dtype, x.device
+    desc = L.LnDesc(T, d, dtype_code(op), dtype_code(dy.dtype), eps, min_std)
+    lib = L.load()
+    if ws is None:
+        ws = workspace(lib.fpo_layernorm_vjp_workspace(C.byref(desc)), dev)
+    L.check(lib.fpo_layernorm_vjp(
+        C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"), _p(dy, dy.dtype, (T, d), dev, "dy"),
+        _p(dx, F32, (T, d), dev, "dx"), _p(dx_lp, op, (T, d), dev, "dx_lp"), _p(dgain, F32, (d,), dev, "dgain"),
+        _p(dbias, F32, (d,), dev, "dbias"), _p(ws, None, None, dev, "ws"), _nbytes(ws), _stream(dev)))
     return ws

@@ -11,6 +11,7 @@
 
 #include "../../include/fpo.h"
 #include "launch.hpp"
+#include "ns.hpp"
 
 // Scratch of fpo_apply_update_noalloc: a file-scope device array (one copy
 // per GPU, held until the process ends). Host code never passes `scratch`
@@ -456,6 +457,111 @@ hipError_t scratch_address(void** out) {
   return hipSuccess;
 }
 
+// ---------------------------------------------------------------- orthogonalisation
+constexpr int64_t kMaxMatNumel = (int64_t)1 << 29;  // operand bands stay below 2^31 bytes through 32-bit offsets
+
+// The checks of desc and sizes that the workspace queries and the calls share.
+int check_ns(const fpo_ns_desc* d, int64_t n, const int64_t* rows, const int64_t* cols, const char* who) {
+  if (!d || !rows || !cols) return fail(FPO_ERR_NULL, "%s: desc, rows and cols are required", who);
+  if (d->dtype != FPO_F32 && d->dtype != FPO_BF16) return fail(FPO_ERR_DTYPE, "%s: unknown dtype %d", who, (int)d->dtype);
+  if (d->steps < 1 || d->steps > fpo::kNsMaxSteps)
+    return fail(FPO_ERR_ARG, "%s: steps must be in [1, %d]", who, fpo::kNsMaxSteps);
+  if (!(d->eps >= 0.0) || !std::isfinite(d->eps)) return fail(FPO_ERR_ARG, "%s: eps must be finite and >= 0", who);
+  if (n <= 0 || n > fpo::kMaxMats) return fail(FPO_ERR_SHAPE, "%s: n_mats must be in [1, %d]", who, fpo::kMaxMats);
+  for (int64_t i = 0; d->coef && i < 3 * (int64_t)d->steps; ++i)
+    if (!std::isfinite(d->coef[i])) return fail(FPO_ERR_ARG, "%s: coef must be finite", who);
+  if (!fpo::ns_plan(d->steps, d->coef, false).ok)
+    return fail(FPO_ERR_ARG, "%s: these coefficients let a singular value grow past %g", who, fpo::kNsMaxSigma);
+  for (int64_t m = 0; m < n; ++m) {
+    if (rows[m] <= 0 || cols[m] <= 0 || rows[m] % 8 || cols[m] % 8 || rows[m] > kIntMax || cols[m] > kIntMax)
+      return fail(FPO_ERR_SHAPE, "%s: sides of matrix %lld must be positive multiples of 8 (%lld x %lld)", who,
+                  (long long)m, (long long)rows[m], (long long)cols[m]);
+    // (padded sides: the elementwise passes' and products' tiles)
+    if (fpo::ns_pad(rows[m]) > kMaxMatNumel / fpo::ns_pad(cols[m]))
+      return fail(FPO_ERR_UNSUPPORTED, "%s: matrix %lld has more than 2^29 entries (sides rounded up to 64)", who,
+                  (long long)m);
+  }
+  return FPO_OK;
+}
+
+// The call's matrices in batches of equal (shorter, longer) side, equal sizes in the
+// caller's order, at most ns_batch_limit to a batch: f(batch, indices).
+template <class F>
+int each_ns_batch(int64_t n, const int64_t* rows, const int64_t* cols, F&& f) {
+  bool done[fpo::kMaxMats] = {};
+  for (int64_t i = 0; i < n; ++i) {
+    if (done[i]) continue;
+    const int64_t s = std::min(rows[i], cols[i]), l = std::max(rows[i], cols[i]);
+    int ids[fpo::kMaxMats], count = 0;
+    for (int64_t j = i; j < n; ++j)
+      if (!done[j] && std::min(rows[j], cols[j]) == s && std::max(rows[j], cols[j]) == l) {
+        ids[count++] = (int)j;
+        done[j] = true;
+      }
+    const int parts = (int)ceil_div(count, fpo::ns_batch_limit(s, l));
+    for (int p = 0, at = 0; p < parts; ++p) {
+      const int c = (count - at) / (parts - p);  // equal parts
+      fpo::NsBatch b{};
+      b.count = c;
+      b.n = s;
+      b.m = l;
+      for (int k = 0; k < c; ++k) {
+        b.id[k] = ids[at + k];
+        if (rows[ids[at + k]] > cols[ids[at + k]]) b.tall |= (uint64_t)1 << k;
+      }
+      at += c;
+      if (int e = f(b)) return e;
+    }
+  }
+  return FPO_OK;
+}
+
+// The batches run one after the other in the same workspace.
+size_t ns_ws(bool bf16, int64_t n, const int64_t* rows, const int64_t* cols) {
+  size_t need = 0;
+  each_ns_batch(n, rows, cols, [&](const fpo::NsBatch& b) {
+    need = std::max(need, fpo::ns_workspace(b.n, b.m, b.count, bf16));
+    return FPO_OK;
+  });
+  return need;
+}
+
+int check_muon(const fpo_muon* o) {
+  if (!o) return fail(FPO_ERR_NULL, "fpo_muon_update: opt is NULL");
+  if (!(o->lr >= 0.0) || !std::isfinite(o->lr)) return fail(FPO_ERR_ARG, "fpo_muon_update: lr must be finite and >= 0");
+  if (!(o->momentum >= 0.0 && o->momentum <= 1.0))
+    return fail(FPO_ERR_ARG, "fpo_muon_update: momentum must be in [0, 1]");
+  if (!(o->weight_decay >= 0.0) || !std::isfinite(o->weight_decay))
+    return fail(FPO_ERR_ARG, "fpo_muon_update: weight_decay must be finite and >= 0");
+  if (!std::isfinite(o->clip_frac)) return fail(FPO_ERR_ARG, "fpo_muon_update: clip_frac must be finite");
+  if (o->step < 1) return fail(FPO_ERR_ARG, "fpo_muon_update: step is 1-based (got %lld)", (long long)o->step);
+  if (o->nesterov != 0 && o->nesterov != 1) return fail(FPO_ERR_ARG, "fpo_muon_update: nesterov must be 0 or 1");
+  if (o->scale < FPO_MUON_SCALE_NONE || o->scale > FPO_MUON_SCALE_RMS)
+    return fail(FPO_ERR_ARG, "fpo_muon_update: unknown scale %d", (int)o->scale);
+  if (o->clip_target != FPO_CLIP_GRADIENT && o->clip_target != FPO_CLIP_UPDATE)
+    return fail(FPO_ERR_ARG, "fpo_muon_update: unknown clip_target %d", (int)o->clip_target);
+  return FPO_OK;
+}
+
+// ---------------------------------------------------------------- layer norm
+int check_ln(const fpo_ln_desc* d, const char* who) {
+  if (!d) return fail(FPO_ERR_NULL, "%s: desc is NULL", who);
+  if ((d->dtype != FPO_F32 && d->dtype != FPO_BF16) || (d->dy_dtype != FPO_F32 && d->dy_dtype != FPO_BF16))
+    return fail(FPO_ERR_DTYPE, "%s: unknown dtype %d / %d", who, (int)d->dtype, (int)d->dy_dtype);
+  if (d->T <= 0 || d->d <= 0 || d->d % 8 || d->T > kMaxTokens || d->d > kMaxHidden)
+    return fail(FPO_ERR_SHAPE, "%s: T must be in [1, %lld], d a multiple of 8 in [8, %lld] (T=%lld d=%lld)", who,
+                (long long)kMaxTokens, (long long)kMaxHidden, (long long)d->T, (long long)d->d);
+  if (!(d->eps >= 0.f) || !std::isfinite(d->eps)) return fail(FPO_ERR_ARG, "%s: eps must be finite and >= 0", who);
+  if (!(d->min_std >= 0.f) || !std::isfinite(d->min_std))
+    return fail(FPO_ERR_ARG, "%s: min_std must be finite and >= 0", who);
+  return FPO_OK;
+}
+
+size_t ln_vjp_ws(const fpo_ln_desc& d) {
+  const int64_t n = fpo::ln_vjp_blocks(d.T, d.d);
+  return n > 1 ? (size_t)round_up(2 * n * d.d * 4, kAlign) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -792,6 +898,155 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A, con
   C.stream = stream;
   hipError_t e = fpo::launch_cosine(C);
   if (e != hipSuccess) return hip_fail(e, "fpo_cosine launch");
+  return FPO_OK;
+}
+
+size_t fpo_orthogonalize_workspace(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* rows,
+                                   const int64_t* cols) {
+  if (check_ns(desc, n_mats, rows, cols, "fpo_orthogonalize")) return 0;
+  return ns_ws(desc->dtype == FPO_BF16, n_mats, rows, cols);
+}
+
+int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* rows, const int64_t* cols,
+                      const void* const* M, void* const* O, void* ws, size_t ws_bytes, void* stream) {
+  if (int e = check_ns(desc, n_mats, rows, cols, "fpo_orthogonalize")) return e;
+  if (!M || !O) return fail(FPO_ERR_NULL, "fpo_orthogonalize: M and O are required");
+  for (int64_t m = 0; m < n_mats; ++m) {
+    if (!M[m] || !O[m]) return fail(FPO_ERR_NULL, "fpo_orthogonalize: NULL buffer for matrix %lld", (long long)m);
+    if (!aligned(M[m], 16) || !aligned(O[m], 16))
+      return fail(FPO_ERR_ARG, "fpo_orthogonalize: buffers of matrix %lld must be 16-byte aligned", (long long)m);
+  }
+  const bool bf16 = desc->dtype == FPO_BF16;
+  if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_orthogonalize")) return e;
+  fpo::NsLaunch L{};
+  L.steps = desc->steps;
+  L.coef = desc->coef;
+  L.bf16 = bf16;
+  L.eps = desc->eps;
+  L.ws = ws;
+  L.stream = stream;
+  return each_ns_batch(n_mats, rows, cols, [&](fpo::NsBatch& b) {
+    for (int k = 0; k < b.count; ++k) {
+      b.x[k] = M[b.id[k]];
+      b.o[k] = O[b.id[k]];
+    }
+    const hipError_t e = fpo::launch_ns(L, b);
+    return e != hipSuccess ? hip_fail(e, "fpo_orthogonalize launch") : (int)FPO_OK;
+  });
+}
+
+size_t fpo_muon_update_workspace(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, const int64_t* cols) {
+  if (check_muon(opt) || check_ns(&opt->ns, n_mats, rows, cols, "fpo_muon_update")) return 0;
+  return ns_ws(opt->ns.dtype == FPO_BF16, n_mats, rows, cols);
+}
+
+int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, const int64_t* cols,
+                    const float* const* grad, const double* grad_sumsq, const fpo_update_bufs* upd, void* ws,
+                    size_t ws_bytes, void* stream) {
+  if (int e = check_muon(opt)) return e;
+  if (int e = check_ns(&opt->ns, n_mats, rows, cols, "fpo_muon_update")) return e;
+  const bool clip = opt->clip_frac > 0.0, clip_update = clip && opt->clip_target == FPO_CLIP_UPDATE;
+  if (!grad || !upd || !upd->W_master) return fail(FPO_ERR_NULL, "fpo_muon_update: grad and upd->W_master are required");
+  if (clip && (!upd->W_sumsq || (!clip_update && !grad_sumsq)))
+    return fail(FPO_ERR_NULL, "fpo_muon_update: the clip needs W_sumsq, and grad_sumsq when it bounds the gradient");
+  const bool bf16 = opt->ns.dtype == FPO_BF16;
+  for (int64_t m = 0; m < n_mats; ++m) {
+    const void* lp = upd->W_lp ? upd->W_lp[m] : nullptr;
+    const float* st = upd->state1 ? upd->state1[m] : nullptr;
+    if (!grad[m] || !upd->W_master[m] || (!st && opt->momentum != 0.0))
+      return fail(FPO_ERR_NULL, "fpo_muon_update: NULL buffer for matrix %lld", (long long)m);
+    if (!aligned(grad[m], 16) || !aligned(upd->W_master[m], 16) || !aligned(st, 16) || !aligned(lp, bf16 ? 8 : 16))
+      return fail(FPO_ERR_ARG, "fpo_muon_update: buffers of matrix %lld must be 16-byte aligned (bf16 W_lp: 8)",
+                  (long long)m);
+  }
+  if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_muon_update")) return e;
+  fpo::NsLaunch L{};
+  L.steps = opt->ns.steps;
+  L.coef = opt->ns.coef;
+  L.bf16 = bf16;
+  L.eps = opt->ns.eps;
+  L.muon = true;
+  L.first = opt->step == 1;
+  L.nesterov = opt->nesterov != 0;
+  L.momentum = (float)opt->momentum;
+  L.clip_frac = clip ? opt->clip_frac : 0.0;
+  L.clip_update = clip_update;
+  L.lr = opt->lr;
+  L.weight_decay = opt->weight_decay;
+  L.scale = opt->scale;
+  L.grad_sumsq = grad_sumsq;
+  L.W_sumsq = upd->W_sumsq;
+  L.clip_scale = upd->clip_scale;
+  L.ws = ws;
+  L.stream = stream;
+  return each_ns_batch(n_mats, rows, cols, [&](fpo::NsBatch& b) {
+    for (int k = 0; k < b.count; ++k) {
+      const int m = b.id[k];
+      b.grad[k] = grad[m];
+      b.W[k] = upd->W_master[m];
+      b.W_lp[k] = upd->W_lp ? upd->W_lp[m] : nullptr;
+      b.state[k] = upd->state1 ? upd->state1[m] : nullptr;
+    }
+    const hipError_t e = fpo::launch_ns(L, b);
+    return e != hipSuccess ? hip_fail(e, "fpo_muon_update launch") : (int)FPO_OK;
+  });
+}
+
+int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, const void* bias, void* y, float* mean,
+                  float* rstd, void* stream) {
+  if (int e = check_ln(desc, "fpo_layernorm")) return e;
+  if (!x || !y) return fail(FPO_ERR_NULL, "fpo_layernorm: x and y are required");
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gain, 16) || !aligned(bias, 16))
+    return fail(FPO_ERR_ARG, "fpo_layernorm: tensors must be 16-byte aligned");
+  fpo::LnLaunch L{};
+  L.bf16 = desc->dtype == FPO_BF16;
+  L.T = desc->T;
+  L.d = desc->d;
+  L.eps = desc->eps;
+  L.x = x;
+  L.gain = gain;
+  L.bias = bias;
+  L.y = y;
+  L.mean = mean;
+  L.rstd = rstd;
+  L.stream = stream;
+  const hipError_t e = fpo::launch_layernorm(L);
+  if (e != hipSuccess) return hip_fail(e, "fpo_layernorm launch");
+  return FPO_OK;
+}
+
+size_t fpo_layernorm_vjp_workspace(const fpo_ln_desc* desc) {
+  if (check_ln(desc, "fpo_layernorm_vjp")) return 0;
+  return ln_vjp_ws(*desc);
+}
+
+int fpo_layernorm_vjp(const fpo_ln_desc* desc, const void* x, const void* gain, const void* dy, float* dx,
+                      void* dx_lp, float* dgain, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+  if (int e = check_ln(desc, "fpo_layernorm_vjp")) return e;
+  if (!x || !dy) return fail(FPO_ERR_NULL, "fpo_layernorm_vjp: x and dy are required");
+  if (!dx && !dx_lp && !dgain && !dbias) return fail(FPO_ERR_NULL, "fpo_layernorm_vjp: no output is asked for");
+  for (const void* p : {x, gain, dy, (const void*)dx, (const void*)dx_lp, (const void*)dgain, (const void*)dbias})
+    if (!aligned(p, 16)) return fail(FPO_ERR_ARG, "fpo_layernorm_vjp: tensors must be 16-byte aligned");
+  if (dgain || dbias)
+    if (int e = check_ws(ws, ws_bytes, ln_vjp_ws(*desc), "fpo_layernorm_vjp")) return e;
+  fpo::LnLaunch L{};
+  L.bf16 = desc->dtype == FPO_BF16;
+  L.dy_bf16 = desc->dy_dtype == FPO_BF16;
+  L.T = desc->T;
+  L.d = desc->d;
+  L.eps = desc->eps;
+  L.min_std = desc->min_std;
+  L.x = x;
+  L.gain = gain;
+  L.dy = dy;
+  L.dx = dx;
+  L.dx_lp = dx_lp;
+  L.dgain = dgain;
+  L.dbias = dbias;
+  L.part = (float*)ws;
+  L.stream = stream;
+  const hipError_t e = fpo::launch_layernorm_vjp(L);
+  if (e != hipSuccess) return hip_fail(e, "fpo_layernorm_vjp launch");
   return FPO_OK;
 }
 

@@ -1,4 +1,4 @@
-// bf16 MFMA tile core with a 2-stage LDS ring fed by LDS-DMA buffer loads
+// 16-bit (bf16, or fp16 with F16) MFMA tile core with a 2-stage LDS ring fed by LDS-DMA buffer loads
 // (gfx950 buffer_load_dwordx4 ... lds). One workgroup of 4 waves (2 x 2)
 // computes a 256 x 256 tile of C = A B, A K-contiguous ([M][K]), B either
 // N-contiguous ([K][N]) or K-contiguous ([N][K], "Bt"). K advances 64 per
@@ -289,26 +289,33 @@ struct Pipe2 {
   }
 };
 
+// One MFMA of 32 x 32 x 16 over bf16 operands, or fp16 ones (the same rate).
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma_16bit(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0,
+                                                  0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+}
+
 #define FPO_SB() __builtin_amdgcn_sched_barrier(0)
 
 // One MFMA group (fragment row f of K step with operands b): the four MFMAs
 // with up to four items of other work placed one after each (sched_barrier
 // keeps the order: with one wave per SIMD the MFMA pipe idles whenever the
 // wave stalls on a burst of other issue).
-template <class X0, class X1, class X2, class X3>
+template <bool F16, class X0, class X1, class X2, class X3>
 __device__ __forceinline__ void mfma_group(f32x16 (&acc)[4][4], int f, u32x4 a, const u32x4 (&b)[4],
                                            X0 x0, X1 x1, X2 x2, X3 x3) {
-  acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, b[0]), acc[f][0], 0, 0, 0);
+  acc[f][0] = mfma_16bit<F16>(a, b[0], acc[f][0]);
   FPO_SB(); x0(); FPO_SB();
-  acc[f][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, b[1]), acc[f][1], 0, 0, 0);
+  acc[f][1] = mfma_16bit<F16>(a, b[1], acc[f][1]);
   FPO_SB(); x1(); FPO_SB();
-  acc[f][2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, b[2]), acc[f][2], 0, 0, 0);
+  acc[f][2] = mfma_16bit<F16>(a, b[2], acc[f][2]);
   FPO_SB(); x2(); FPO_SB();
-  acc[f][3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                      __builtin_bit_cast(bf16x8, b[3]), acc[f][3], 0, 0, 0);
+  acc[f][3] = mfma_16bit<F16>(a, b[3], acc[f][3]);
   FPO_SB(); x3(); FPO_SB();
 }
 
@@ -321,7 +328,7 @@ __device__ __forceinline__ void mfma_group(f32x16 (&acc)[4][4], int f, u32x4 a, 
 // barrier). After group 13: wait for tile j+1's copies, barrier. Groups 14, 15
 // read tile j+1's first operands and issue tile j+2's copies 0..3 into the
 // stage just released.
-template <bool BNC, bool FAST>
+template <bool BNC, bool FAST, bool F16>
 __device__ __forceinline__ void gemm2_iter(const Pipe2<BNC>& p, G2Smem& sm, f32x16 (&acc)[4][4],
                                            u32x4 (&bc)[4], u32x4 (&a)[2], int j, int kt0) {
   const u32x4* cur = sm.s + (j & 1) * G2::STAGE_CHUNKS;
@@ -333,43 +340,43 @@ __device__ __forceinline__ void gemm2_iter(const Pipe2<BNC>& p, G2Smem& sm, f32x
   u32x4 bq[4], bn[4];
   u32x4 a2, a3, a4, a5, a6, a7, a8, a9, a10, a11, a12, a13, a14, a15;
   // ---- K step 0
-  mfma_group(acc, 0, a[0], bc, [&] { a2 = p.read_a(cur, 2, 0); }, [&] { p.template issue<FAST>(s1, t1, 4); },
+  mfma_group<F16>(acc, 0, a[0], bc, [&] { a2 = p.read_a(cur, 2, 0); }, [&] { p.template issue<FAST>(s1, t1, 4); },
              [&] { p.read_b(cur, 1, 0, raw, bq); }, [&] { p.template issue<FAST>(s1, t1, 5); });
-  mfma_group(acc, 1, a[1], bc, [&] { a3 = p.read_a(cur, 3, 0); }, [&] { p.template issue<FAST>(s1, t1, 6); },
+  mfma_group<F16>(acc, 1, a[1], bc, [&] { a3 = p.read_a(cur, 3, 0); }, [&] { p.template issue<FAST>(s1, t1, 6); },
              [&] { p.read_b(cur, 1, 1, raw, bq); }, [&] { p.template issue<FAST>(s1, t1, 7); });
-  mfma_group(acc, 2, a2, bc, [&] { a4 = p.read_a(cur, 0, 1); }, [&] { p.template issue<FAST>(s1, t1, 8); },
+  mfma_group<F16>(acc, 2, a2, bc, [&] { a4 = p.read_a(cur, 0, 1); }, [&] { p.template issue<FAST>(s1, t1, 8); },
              [&] { Pipe2<BNC>::pack_b(raw, bq, bn, 0); }, [&] { p.template issue<FAST>(s1, t1, 9); });
-  mfma_group(acc, 3, a3, bc, [&] { a5 = p.read_a(cur, 1, 1); }, [&] { p.template issue<FAST>(s1, t1, 10); },
+  mfma_group<F16>(acc, 3, a3, bc, [&] { a5 = p.read_a(cur, 1, 1); }, [&] { p.template issue<FAST>(s1, t1, 10); },
              [&] { Pipe2<BNC>::pack_b(raw, bq, bn, 1); }, [&] { p.template issue<FAST>(s1, t1, 11); });
   // ---- K step 1
-  mfma_group(acc, 0, a4, bn, [&] { a6 = p.read_a(cur, 2, 1); }, [&] { p.template issue<FAST>(s1, t1, 12); },
+  mfma_group<F16>(acc, 0, a4, bn, [&] { a6 = p.read_a(cur, 2, 1); }, [&] { p.template issue<FAST>(s1, t1, 12); },
              [&] { p.read_b(cur, 2, 0, raw, bq); }, [&] { p.template issue<FAST>(s1, t1, 13); });
-  mfma_group(acc, 1, a5, bn, [&] { a7 = p.read_a(cur, 3, 1); }, [&] { p.template issue<FAST>(s1, t1, 14); },
+  mfma_group<F16>(acc, 1, a5, bn, [&] { a7 = p.read_a(cur, 3, 1); }, [&] { p.template issue<FAST>(s1, t1, 14); },
              [&] { p.read_b(cur, 2, 1, raw, bq); }, [&] { p.template issue<FAST>(s1, t1, 15); });
-  mfma_group(acc, 2, a6, bn, [&] { a8 = p.read_a(cur, 0, 2); }, nop,
+  mfma_group<F16>(acc, 2, a6, bn, [&] { a8 = p.read_a(cur, 0, 2); }, nop,
              [&] { Pipe2<BNC>::pack_b(raw, bq, bc, 0); }, nop);
-  mfma_group(acc, 3, a7, bn, [&] { a9 = p.read_a(cur, 1, 2); }, nop,
+  mfma_group<F16>(acc, 3, a7, bn, [&] { a9 = p.read_a(cur, 1, 2); }, nop,
              [&] { Pipe2<BNC>::pack_b(raw, bq, bc, 1); }, nop);
   // ---- K step 2 (operands in bc)
-  mfma_group(acc, 0, a8, bc, [&] { a10 = p.read_a(cur, 2, 2); }, nop,
+  mfma_group<F16>(acc, 0, a8, bc, [&] { a10 = p.read_a(cur, 2, 2); }, nop,
              [&] { p.read_b(cur, 3, 0, raw, bq); }, nop);
-  mfma_group(acc, 1, a9, bc, [&] { a11 = p.read_a(cur, 3, 2); }, nop,
+  mfma_group<F16>(acc, 1, a9, bc, [&] { a11 = p.read_a(cur, 3, 2); }, nop,
              [&] { p.read_b(cur, 3, 1, raw, bq); }, nop);
-  mfma_group(acc, 2, a10, bc, [&] { a12 = p.read_a(cur, 0, 3); }, [&] { a14 = p.read_a(cur, 2, 3); },
+  mfma_group<F16>(acc, 2, a10, bc, [&] { a12 = p.read_a(cur, 0, 3); }, [&] { a14 = p.read_a(cur, 2, 3); },
              [&] { Pipe2<BNC>::pack_b(raw, bq, bn, 0); }, nop);
-  mfma_group(acc, 3, a11, bc, [&] { a13 = p.read_a(cur, 1, 3); }, [&] { a15 = p.read_a(cur, 3, 3); },
+  mfma_group<F16>(acc, 3, a11, bc, [&] { a13 = p.read_a(cur, 1, 3); }, [&] { a15 = p.read_a(cur, 3, 3); },
              [&] { Pipe2<BNC>::pack_b(raw, bq, bn, 1); }, nop);
   // ---- K step 3 (operands in bn)
-  mfma_group(acc, 0, a12, bn, nop, nop, nop, nop);
-  mfma_group(acc, 1, a13, bn, nop, nop, nop, [&] {
+  mfma_group<F16>(acc, 0, a12, bn, nop, nop, nop, nop);
+  mfma_group<F16>(acc, 1, a13, bn, nop, nop, nop, [&] {
     // every read of this stage is complete and tile j+1 has landed
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     wait_vmcnt<0>();
     stage_barrier();
   });
-  mfma_group(acc, 2, a14, bn, [&] { p.read_b(nxt, 0, 0, raw, bq); }, [&] { a[0] = p.read_a(nxt, 0, 0); },
+  mfma_group<F16>(acc, 2, a14, bn, [&] { p.read_b(nxt, 0, 0, raw, bq); }, [&] { a[0] = p.read_a(nxt, 0, 0); },
              [&] { p.read_b(nxt, 0, 1, raw, bq); }, [&] { p.template issue<FAST>(s2, t2, 0); });
-  mfma_group(acc, 3, a15, bn, [&] { a[1] = p.read_a(nxt, 1, 0); }, [&] { p.template issue<FAST>(s2, t2, 1); },
+  mfma_group<F16>(acc, 3, a15, bn, [&] { a[1] = p.read_a(nxt, 1, 0); }, [&] { p.template issue<FAST>(s2, t2, 1); },
              [&] { p.template issue<FAST>(s2, t2, 2); }, [&] { p.template issue<FAST>(s2, t2, 3); });
   Pipe2<BNC>::pack_b(raw, bq, bc, 0);
   Pipe2<BNC>::pack_b(raw, bq, bc, 1);
@@ -381,7 +388,7 @@ __device__ __forceinline__ void gemm2_iter(const Pipe2<BNC>& p, G2Smem& sm, f32x
 // Copies are issued for every iteration (beyond the last tile they read
 // zeros, or the next split's data, into a stage no longer needed), so every
 // wait is the same: vmcnt(0) at the barrier of each tile.
-template <bool BNC, bool FAST = false>
+template <bool BNC, bool FAST = false, bool F16 = false>
 __device__ __forceinline__ void gemm2_mainloop(G2Smem& sm, f32x16 (&acc)[4][4], const Operand& A,
                                                const Operand& B, int M_rem, int N_rem, int K,
                                                int kt0, int kt1) {
@@ -404,7 +411,7 @@ __device__ __forceinline__ void gemm2_mainloop(G2Smem& sm, f32x16 (&acc)[4][4], 
   a[1] = p.read_a(sm.s, 1, 0);
   Pipe2<BNC>::pack_b(raw, bq, bc, 0);
   Pipe2<BNC>::pack_b(raw, bq, bc, 1);
-  for (int j = 0; j < n; ++j) gemm2_iter<BNC, FAST>(p, sm, acc, bc, a, j, kt0);
+  for (int j = 0; j < n; ++j) gemm2_iter<BNC, FAST, F16>(p, sm, acc, bc, a, j, kt0);
   wait_vmcnt<0>();
   __syncthreads();
 }

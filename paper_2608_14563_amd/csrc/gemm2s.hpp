@@ -1,4 +1,4 @@
-// bf16 MFMA core for 128 x 128 tiles, for launches whose 256 x 256 tiles
+// 16-bit (bf16, or fp16 with F16) MFMA core for 128 x 128 tiles, for launches whose 256 x 256 tiles
 // (gemm2.hpp) would leave most CUs without one. Same operands (A K-contiguous,
 // B N-contiguous or K-contiguous), the same 64-deep K stages, LDS-DMA copies and
 // chunk swizzle, and v_mfma_f32_32x32x16_bf16; 4 waves.
@@ -167,9 +167,9 @@ __device__ __forceinline__ void read_step(Frags2S<BNC>& fr, const Pipe2S<BNC>& p
   }
 }
 
-// C tile accumulated over K tiles [kt0, kt1); acc starts at zero. Ends with a
+// C tile accumulated over K tiles [kt0, kt1), added to acc. Ends with a
 // barrier and no copy in flight, so the caller may reuse LDS.
-template <bool BNC>
+template <bool BNC, bool F16 = false>
 __device__ __forceinline__ void gemm2s_mainloop(G2SSmem& sm, f32x16 (&acc)[G2SWave<BNC>::FM][G2SWave<BNC>::FN],
                                                 const Operand& A, const Operand& B, int M_rem, int N_rem, int K,
                                                 int kt0, int kt1) {
@@ -217,9 +217,7 @@ __device__ __forceinline__ void gemm2s_mainloop(G2SSmem& sm, f32x16 (&acc)[G2SWa
         if (m & 1) p.issue(j % G2S::NST, 2 * h + (m >> 1));
         __builtin_amdgcn_sched_barrier(0);
         const int f = m / W::FN, i = m % W::FN;
-        acc[f][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, cur.a[h][f]),
-                                                            __builtin_bit_cast(bf16x8, cur.b[h][i]), acc[f][i], 0, 0,
-                                                            0);
+        acc[f][i] = mfma_16bit<F16>(cur.a[h][f], cur.b[h][i], acc[f][i]);
         __builtin_amdgcn_sched_barrier(0);
       }
   };

@@ -1,0 +1,422 @@
+// Layer norm over the last dimension, forward and VJP with the gradients of gain and
+// bias (fpo_layernorm, fpo_layernorm_vjp):
+//   mu = mean x, sigma = sqrt(mean (x - mu)^2 + eps), y = gain (x - mu) / sigma + bias
+//   v = gain dy, sigma~ = max(sigma, min_std), x^ = (x - mu) / sigma~
+//   dx = (v - mean v - x^ mean(v x^)) / sigma~
+//   dgain = sum_t dy (x - mu) / sigma, dbias = sum_t dy
+// Both are bound by HBM: a row is read once into registers, its statistics are two
+// reductions over the lanes that share it (the squares are of differences from the
+// mean, so that a large mean costs no digits), and everything else is elementwise.
+//
+// A row is shared by 64 lanes (d up to 2048), 256 (up to 8192) or 1024 (up to 16384), each
+// holding up to four chunks of eight neighbouring elements; longer rows are read again for
+// every reduction. In the VJP a workgroup takes every grid-th row (group of four for 64 lanes)
+// and keeps its columns' sums of the two parameter gradients in registers; the workgroups'
+// sums go to the workspace and a second launch adds them in a fixed order (no atomics:
+// the same input gives the same bits). The next row is loaded before the current one's
+// reductions.
+#include "common.hpp"
+#include "launch.hpp"
+#include "prof.hpp"
+
+namespace fpo {
+
+namespace {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+
+template <typename T>
+struct Raw8;  // eight stored elements
+template <>
+struct Raw8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4*>(p);
+    b = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ __forceinline__ f32x8 get() const { return f32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}; }
+};
+template <>
+struct Raw8<uint16_t> {
+  u32x4 a;
+  __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ f32x8 get() const {
+    return f32x8{bf16_lo(a.x), bf16_hi(a.x), bf16_lo(a.y), bf16_hi(a.y),
+                 bf16_lo(a.z), bf16_hi(a.z), bf16_lo(a.w), bf16_hi(a.w)};
+  }
+};
+__device__ __forceinline__ void store8(float* p, f32x8 v) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store8(uint16_t* p, f32x8 v) {
+  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                       pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ float sum8(f32x8 v) {
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
+// Sum over the LANES lanes of a row; 64 lanes: within the wave, else the workgroup is one
+// row's. `red` holds 2 floats a wave.
+template <int LANES>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  if constexpr (LANES == 64) return wave_sum(v);
+  else return block_sum(v, red);
+}
+template <int LANES>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float* red) {
+  if constexpr (LANES == 64) {
+    a = wave_sum(a);
+    b = wave_sum(b);
+  } else {
+    block_sum2(a, b, red);
+  }
+}
+
+constexpr int ln_threads(int lanes) { return lanes == 1024 ? 1024 : 256; }
+
+// NV: chunks a lane (of 8 elements, LANES chunks apart); 0: any number, read again.
+template <typename T, int LANES, int NV>
+__global__ __launch_bounds__(ln_threads(LANES)) void ln_forward_kernel(const T* __restrict__ x, const T* __restrict__ gain,
+                                                                      const T* __restrict__ bias, int64_t rows, int d,
+                                                                      float eps, T* __restrict__ y,
+                                                                      float* __restrict__ mean_out,
+                                                                      float* __restrict__ rstd_out) {
+  __shared__ float red[32];
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+  constexpr int SLOTS = ln_threads(LANES) / LANES;
+  const int nc = d / 8;
+  const float inv_d = 1.f / (float)d;
+  // (with several slots a row's lanes are a whole wave, and nothing in the loop is a barrier)
+  for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot; row < rows; row += (int64_t)gridDim.x * SLOTS) {
+    const T* xr = x + row * d;
+    f32x8 v[NV ? NV : 1];
+    float s = 0.f;
+    auto each = [&](auto&& f) {  // f(chunk, values): every chunk of the lane
+      if constexpr (NV > 0) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (lane + k * LANES < nc) f(lane + k * LANES, v[k]);
+      } else {
+        for (int c = lane; c < nc; c += LANES) {
+          Raw8<T> r;
+          r.load(xr + 8 * c);
+          f(c, r.get());
+        }
+      }
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (lane + k * LANES < nc) {
+          Raw8<T> r;
+          r.load(xr + 8 * (lane + k * LANES));
+          v[k] = r.get();
+        }
+    }
+    each([&](int, f32x8 t) { s += sum8(t); });
+    const float mean = row_sum<LANES>(s, red) * inv_d;
+    s = 0.f;
+    each([&](int, f32x8 t) {
+      t -= mean;
+      s += sum8(t * t);
+    });
+    const float rstd = 1.f / sqrtf(row_sum<LANES>(s, red) * inv_d + eps);
+    each([&](int c, f32x8 t) {
+      t = (t - mean) * rstd;
+      if (gain) {
+        Raw8<T> g;
+        g.load(gain + 8 * c);
+        t *= g.get();
+      }
+      if (bias) {
+        Raw8<T> b;
+        b.load(bias + 8 * c);
+        t += b.get();
+      }
+      store8(y + row * d + 8 * c, t);
+    });
+    if (lane == 0) {
+      if (mean_out) mean_out[row] = mean;
+      if (rstd_out) rstd_out[row] = rstd;
+    }
+  }
+}
+
+struct LnVjp {
+  const void* x;
+  const void* gain;
+  const void* dy;
+  float* dx;
+  void* dx_lp;
+  float* pgain;  // [gridDim.x][d] sums of a workgroup's rows (the results, with one workgroup), or null
+  float* pbias;
+  int64_t rows;
+  int d;
+  float eps, min_std;
+};
+
+// PARAM: sums for dgain and dbias are kept, in registers, or with NV == 0 (very long
+// rows) in the workgroup's partials themselves, each entry only ever touched by one lane.
+template <typename T, typename TD, int LANES, int NV, bool PARAM>
+__global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
+  constexpr int SLOTS = ln_threads(LANES) / LANES;
+  constexpr int NR = NV ? NV : 1;
+  constexpr bool AHEAD = NV > 0 && LANES < 1024;  // (1024 lanes have no registers left for it)
+  __shared__ float red[32];
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+  const T* x = (const T*)a.x;
+  const TD* dy = (const TD*)a.dy;
+  const T* gain = (const T*)a.gain;
+  T* dx_lp = (T*)a.dx_lp;
+  const int d = a.d, nc = d / 8;
+  const float inv_d = 1.f / (float)d;
+  const int64_t step = (int64_t)gridDim.x * SLOTS;
+  f32x8 pg[PARAM ? NR : 1], pb[PARAM ? NR : 1];
+  if constexpr (PARAM) {
+#pragma unroll
+    for (int k = 0; k < NR; ++k) pg[k] = pb[k] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  }
+  Raw8<T> rx[NR];
+  Raw8<TD> rd[NR];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+      if (lane + k * LANES < nc) {
+        rx[k].load(x + row * d + 8 * (lane + k * LANES));
+        rd[k].load(dy + row * d + 8 * (lane + k * LANES));
+      }
+  };
+  auto gain8 = [&](int c) {
+    f32x8 g = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    if (gain) {
+      Raw8<T> r;
+      r.load(gain + 8 * c);
+      g = r.get();
+    }
+    return g;
+  };
+  int64_t row = (int64_t)blockIdx.x * SLOTS + slot;
+  if constexpr (AHEAD) {
+    if (row < a.rows) fetch(row);
+  }
+  // with several slots a row's lanes are whole waves and nothing in the loop is a barrier
+  for (; row < a.rows; row += step) {
+    f32x8 vx[NR], vd[NR];
+    float s = 0.f;
+    auto each = [&](auto&& f) {  // f(chunk, k, x, dy)
+      if constexpr (NV > 0) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (lane + k * LANES < nc) f(lane + k * LANES, k, vx[k], vd[k]);
+      } else {
+        for (int c = lane; c < nc; c += LANES) {
+          Raw8<T> r;
+          Raw8<TD> q;
+          r.load(x + row * d + 8 * c);
+          q.load(dy + row * d + 8 * c);
+          f(c, 0, r.get(), q.get());
+        }
+      }
+    };
+    if constexpr (NV > 0) {
+      if constexpr (!AHEAD) fetch(row);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        vx[k] = rx[k].get();
+        vd[k] = rd[k].get();
+      }
+    }
+    if constexpr (AHEAD) {
+      if (row + step < a.rows) fetch(row + step);
+    }
+    each([&](int, int, f32x8 t, f32x8) { s += sum8(t); });
+    const float mean = row_sum<LANES>(s, red) * inv_d;
+    s = 0.f;
+    each([&](int, int, f32x8 t, f32x8) {
+      t -= mean;
+      s += sum8(t * t);
+    });
+    const float sigma = sqrtf(row_sum<LANES>(s, red) * inv_d + a.eps);
+    const float rstd = 1.f / sigma, inv = 1.f / fmaxf(sigma, a.min_std);
+    float c1 = 0.f, c2 = 0.f;
+    each([&](int c, int, f32x8 t, f32x8 g) {
+      const f32x8 v = g * gain8(c);
+      c1 += sum8(v);
+      c2 += sum8(v * ((t - mean) * inv));
+    });
+    row_sum2<LANES>(c1, c2, red);
+    c1 *= inv_d;
+    c2 *= inv_d;
+    each([&](int c, int k, f32x8 t, f32x8 g) {
+      const f32x8 xc = t - mean;
+      if constexpr (PARAM && NV > 0) {
+        pg[k] += g * (xc * rstd);
+        pb[k] += g;
+      } else if constexpr (PARAM) {
+        const int64_t at = (int64_t)blockIdx.x * d + 8 * c;
+        const bool add = row != (int64_t)blockIdx.x;  // not the workgroup's first row
+        auto keep = [&](float* p, f32x8 w) {
+          if (!p) return;
+          if (add) {
+            Raw8<float> old;
+            old.load(p + at);
+            w += old.get();
+          }
+          store8(p + at, w);
+        };
+        keep(a.pgain, g * (xc * rstd));
+        keep(a.pbias, g);
+      }
+      const f32x8 o = (g * gain8(c) - c1 - xc * inv * c2) * inv;
+      if (a.dx) store8(a.dx + row * d + 8 * c, o);
+      if (dx_lp) store8(dx_lp + row * d + 8 * c, o);
+    });
+  }
+  if constexpr (PARAM && NV > 0) {
+    if constexpr (SLOTS == 1) {
+#pragma unroll
+      for (int k = 0; k < NR; ++k)
+        if (lane + k * LANES < nc) {
+          const int64_t at = (int64_t)blockIdx.x * d + 8 * (lane + k * LANES);
+          if (a.pgain) store8(a.pgain + at, pg[k]);
+          if (a.pbias) store8(a.pbias + at, pb[k]);
+        }
+    } else {  // the four waves' sums, in a fixed order
+      __shared__ f32x8 part[SLOTS][64];
+#pragma unroll
+      for (int k = 0; k < NR; ++k)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          __syncthreads();
+          part[slot][lane] = which ? pb[k] : pg[k];
+          __syncthreads();
+          float* out = which ? a.pbias : a.pgain;
+          if (slot == 0 && out && lane + k * 64 < nc) {
+            f32x8 t = part[0][lane];
+#pragma unroll
+            for (int w = 1; w < SLOTS; ++w) t += part[w][lane];
+            store8(out + (int64_t)blockIdx.x * d + 8 * (lane + k * 64), t);
+          }
+        }
+    }
+  }
+}
+
+// Column sums of the workgroups' partials, dgain with blockIdx.y == 0, dbias with 1: 32
+// columns a workgroup, eight rows of partials at a time, added in double.
+__global__ __launch_bounds__(256) void ln_reduce_kernel(const float* __restrict__ pgain, const float* __restrict__ pbias,
+                                                        int n, int d, float* dgain, float* dbias) {
+  __shared__ double part[8][32];
+  const float* p = blockIdx.y ? pbias : pgain;
+  float* out = blockIdx.y ? dbias : dgain;
+  if (!out) return;
+  const int c = threadIdx.x % 32, r = threadIdx.x / 32, col = blockIdx.x * 32 + c;
+  double s = 0.0;
+  if (col < d)
+    for (int i = r; i < n; i += 8) s += (double)p[(int64_t)i * d + col];
+  part[r][c] = s;
+  __syncthreads();
+  if (r == 0 && col < d) {
+    for (int i = 1; i < 8; ++i) s += part[i][c];
+    out[col] = (float)s;
+  }
+}
+
+constexpr int kLnForwardBlocks = 1 << 20;  // (a grid holds fewer than 2^32 lanes)
+constexpr int kLnBlocks = 2048;      // workgroups of the VJP without parameter gradients
+constexpr int kLnParamBlocks = 512;  // with them: each leaves a row of partials
+
+// How rows of d elements are held: lanes a row and chunks a lane (0: read again).
+struct LnShape {
+  int lanes, nv;
+};
+LnShape ln_shape(int64_t d) {
+  const int64_t nc = d / 8;
+  if (nc <= 64) return {64, 1};
+  if (nc <= 128) return {64, 2};
+  if (nc <= 256) return {64, 4};
+  if (nc <= 512) return {256, 2};
+  if (nc <= 1024) return {256, 4};
+  if (nc <= 2048) return {1024, 2};  // (1024 lanes leave 128 registers each)
+  return {1024, 0};
+}
+
+// f(std::integral_constant lanes, nv) for the shape
+template <class F>
+void with_shape(LnShape s, F&& f) {
+  if (s.lanes == 64 && s.nv == 1) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else if (s.lanes == 64 && s.nv == 2) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+  else if (s.lanes == 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+  else if (s.lanes == 256 && s.nv == 2) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
+  else if (s.lanes == 256) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  else if (s.nv == 2) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+  else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
+}
+
+#define FPO_CHECK_LAUNCH()             \
+  do {                                 \
+    hipError_t e_ = hipGetLastError(); \
+    if (e_ != hipSuccess) return e_;   \
+  } while (0)
+
+template <typename T>
+hipError_t run_forward(const LnLaunch& a) {
+  hipStream_t st = (hipStream_t)a.stream;
+  with_shape(ln_shape(a.d), [&](auto lanes, auto nv) {
+    constexpr int kThreads = ln_threads(lanes), kSlots = kThreads / lanes;
+    FPO_LAUNCH("ln_forward", st,
+               (ln_forward_kernel<T, lanes, nv><<<dim3((unsigned)std::min<int64_t>(ceil_div(a.T, kSlots), kLnForwardBlocks)), dim3(kThreads), 0, st>>>(
+                   (const T*)a.x, (const T*)a.gain, (const T*)a.bias, a.T, (int)a.d, a.eps, (T*)a.y, a.mean, a.rstd)));
+  });
+  FPO_CHECK_LAUNCH();
+  return hipSuccess;
+}
+
+template <typename T, typename TD>
+hipError_t run_vjp(const LnLaunch& a) {
+  hipStream_t st = (hipStream_t)a.stream;
+  const LnShape sh = ln_shape(a.d);
+  const bool param = a.dgain || a.dbias;
+  const int64_t groups = ceil_div(a.T, ln_threads(sh.lanes) / sh.lanes);
+  const int n = param ? ln_vjp_blocks(a.T, a.d) : (int)std::min<int64_t>(groups, kLnBlocks);
+  const bool direct = n == 1;  // one workgroup's sums are the results
+  LnVjp v{a.x, a.gain, a.dy, a.dx, a.dx_lp, nullptr, nullptr, a.T, (int)a.d, a.eps, a.min_std};
+  if (a.dgain) v.pgain = direct ? a.dgain : a.part;
+  if (a.dbias) v.pbias = direct ? a.dbias : a.part + (int64_t)n * a.d;
+  with_shape(sh, [&](auto lanes, auto nv) {
+    if (param)
+      FPO_LAUNCH("ln_vjp", st,
+                 (ln_vjp_kernel<T, TD, lanes, nv, true><<<dim3(n), dim3(ln_threads(lanes)), 0, st>>>(v)));
+    else
+      FPO_LAUNCH("ln_vjp", st,
+                 (ln_vjp_kernel<T, TD, lanes, nv, false><<<dim3(n), dim3(ln_threads(lanes)), 0, st>>>(v)));
+  });
+  FPO_CHECK_LAUNCH();
+  if (param && !direct) {
+    FPO_LAUNCH("ln_reduce", st,
+               ln_reduce_kernel<<<dim3((unsigned)ceil_div(a.d, 32), 2), dim3(256), 0, st>>>(v.pgain, v.pbias, n,
+                                                                                           (int)a.d, a.dgain, a.dbias));
+    FPO_CHECK_LAUNCH();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+int ln_vjp_blocks(int64_t T, int64_t d) {
+  const LnShape s = ln_shape(d);
+  return (int)std::min<int64_t>(ceil_div(T, ln_threads(s.lanes) / s.lanes), kLnParamBlocks);
+}
+
+hipError_t launch_layernorm(const LnLaunch& a) {
+  return a.bf16 ? run_forward<uint16_t>(a) : run_forward<float>(a);
+}
+
+hipError_t launch_layernorm_vjp(const LnLaunch& a) {
+  if (a.bf16) return a.dy_bf16 ? run_vjp<uint16_t, uint16_t>(a) : run_vjp<uint16_t, float>(a);
+  return a.dy_bf16 ? run_vjp<float, uint16_t>(a) : run_vjp<float, float>(a);
+}
+
+}  // namespace fpo

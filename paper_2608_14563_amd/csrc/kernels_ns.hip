@@ -1,0 +1,685 @@
+// Orthogonalisation by Newton-Schulz products and the optimizer step built on it.
+//
+// X = M / (||M||_F + eps), n x m with n <= m (a matrix with more rows than columns is
+// taken transposed); each step X <- a X + b (X X^T) X + c (X X^T)^2 X. Every step is a
+// polynomial of X X^T, so that several steps need X only twice: A = X X^T once, the
+// steps' factors B_j = a I + b A_j + c A_j^2 and A_{j+1} = B_j A_j B_j among n x n
+// matrices, then X <- (B_g ... B_1) X (ns.hpp: groups). All n x n matrices here are
+// symmetric: only the tiles on and under the diagonal are computed, each stored at
+// both places.
+//
+// Number formats. Products take fp16 operands and add in fp32. Every matrix is stored
+// times a power of two that keeps a bound of its spectral norm under 2^13 (ns.hpp), so
+// that fp16's range is no concern and its 11 bits count: with bf16 operands (8 bits)
+// the five-step result of a 512 x 1536 normal matrix is off by 1.1e-2 against 64 bits,
+// with fp16 by 1.3e-3. The matrix instructions run at the same rate. The first X is
+// kept as a pair hi + lo of fp16 for its product with the factors: its small singular
+// values are enlarged most (3.4445^5 = 485 times), and so is its rounding. With float32
+// operands every matrix is such a pair and a product the three hi hi + hi lo + lo hi:
+// 22 to 23 bits at three times the work, where fp32 matrix instructions take 16 times.
+#include "gemm2s.hpp"
+#include "gemm.hpp"
+#include "ns.hpp"
+#include "prof.hpp"
+#include "upd.hpp"
+
+namespace fpo {
+
+namespace {
+
+// A stack of equal matrices in the workspace: fp16, or pairs of fp16 (lo set).
+struct NsMat {
+  uint16_t* hi;
+  uint16_t* lo;
+  int64_t stride;  // elements from one matrix to the next
+};
+
+// One launch of products C = A B over `count` matrices, for one or two sets of operands.
+struct NsGemmArgs {
+  NsMat a[2], b[2], c[2];
+  NsMat e;             // kPoly: A itself, for its linear term
+  int lda, ldb, ldc;
+  int M, N, K;         // padded sizes (multiples of 64)
+  int count, tiles;    // matrices; tiles a matrix
+  int nseg;            // operand halves: 1: hi hi, 2: hi (hi + lo), 3: (hi + lo) (hi + lo) without lo lo
+  float alpha[2];      // by set: C = alpha A B,
+  float beta, diag;    // kPoly: + beta e + diag I
+};
+
+enum { kScale = 0, kPoly = 1 };
+
+__device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+__device__ __forceinline__ float f16_to_f32(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+
+// Tile (tm, tn), tn <= tm, of entry t of the lower triangle taken row by row.
+__device__ __forceinline__ void tri_tile(int t, int& tm, int& tn) {
+  int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+  while (r * (r + 1) / 2 > t) --r;
+  while ((r + 1) * (r + 2) / 2 <= t) ++r;
+  tm = r;
+  tn = t - r * (r + 1) / 2;
+}
+
+template <int EDGE, bool BNC>
+struct NsCore;
+template <bool BNC>
+struct NsCore<256, BNC> {
+  using Smem = G2Smem;
+  using Map = AccMap2<BNC>;
+  static constexpr int FM = 4, FN = 4, VEC = BNC ? 4 : 1;
+};
+template <bool BNC>
+struct NsCore<128, BNC> {
+  using Smem = G2SSmem;
+  using Map = AccMap2S<BNC>;
+  static constexpr int FM = G2SWave<BNC>::FM, FN = G2SWave<BNC>::FN, VEC = 1;
+};
+
+// SYM: C is symmetric, B K-contiguous ([N][K]); only tiles with tn <= tm. Otherwise B
+// is N-contiguous ([K][N]). PAIR: C is stored as hi + lo.
+template <int EDGE, bool FAST, bool SYM, int EPI, bool PAIR>
+__global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
+  constexpr bool BNC = !SYM;
+  using Core = NsCore<EDGE, BNC>;
+  __shared__ typename Core::Smem sm;
+  const int ntm = (g.M + EDGE - 1) / EDGE, ntn = (g.N + EDGE - 1) / EDGE;
+  int mat = blockIdx.x / g.tiles;
+  const int loc = xcd_remap((int)blockIdx.x - mat * g.tiles, g.tiles);
+  const int set = mat / g.count;
+  mat -= set * g.count;
+  int tm, tn;
+  if constexpr (SYM)
+    tri_tile(loc, tm, tn);
+  else
+    grouped_tile(loc, ntm, ntn, 8, tm, tn);
+  tm = to_scalar(tm);
+  tn = to_scalar(tn);
+  mat = to_scalar(mat);
+  const int m0 = tm * EDGE, n0 = tn * EDGE;
+  const NsMat a = set ? g.a[1] : g.a[0], b = set ? g.b[1] : g.b[0], c = set ? g.c[1] : g.c[0];
+  f32x16 acc[Core::FM][Core::FN];
+  if constexpr (EDGE == 256)
+    zero_acc2(acc);
+  else
+    zero_acc2s<BNC>(acc);
+#pragma unroll 1
+  for (int s = 0; s < g.nseg; ++s) {
+    const uint16_t* ap = (s == 2 ? a.lo : a.hi) + mat * a.stride + (int64_t)m0 * g.lda;
+    const uint16_t* bp = (s == 1 ? b.lo : b.hi) + mat * b.stride + (BNC ? (int64_t)n0 : (int64_t)n0 * g.ldb);
+    const Operand A{ap, g.lda, band_bytes(g.M - m0, g.lda)};
+    const Operand B{bp, g.ldb, BNC ? band_bytes(g.K, g.ldb, n0) : band_bytes(g.N - n0, g.ldb)};
+    if constexpr (EDGE == 256)
+      gemm2_mainloop<BNC, FAST, true>(sm, acc, A, B, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
+    else
+      gemm2s_mainloop<BNC, true>(sm, acc, A, B, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
+  }
+  // ---- epilogue
+  const float alpha = set ? g.alpha[1] : g.alpha[0];
+  const typename Core::Map map;
+  uint16_t* ch = c.hi + mat * c.stride;
+  uint16_t* cl = PAIR ? c.lo + mat * c.stride : nullptr;
+  const uint16_t* eh = EPI == kPoly ? g.e.hi + mat * g.e.stride : nullptr;
+  const uint16_t* el = EPI == kPoly && PAIR ? g.e.lo + mat * g.e.stride : nullptr;
+#pragma unroll
+  for (int f = 0; f < Core::FM; ++f)
+#pragma unroll
+    for (int i = 0; i < Core::FN; i += Core::VEC)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = m0 + map.row(f, 4 * q), col = n0 + map.col(i);
+        if (row >= g.M || col >= g.N) continue;  // M and N are multiples of 64: four rows or columns are in or out
+        if constexpr (SYM) {
+          uint16_t h[4], l[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v = alpha * acc[f][i][4 * q + r];
+            const int64_t at = (int64_t)(row + r) * g.ldc + col;
+            if constexpr (EPI == kPoly) {
+              float e = f16_to_f32(eh[at]);
+              if constexpr (PAIR) e += f16_to_f32(el[at]);
+              v = fmaf(g.beta, e, v);
+              if (row + r == col) v += g.diag;
+            }
+            h[r] = to_f16(v);
+            ch[at] = h[r];
+            if constexpr (PAIR) {
+              l[r] = to_f16(v - f16_to_f32(h[r]));
+              cl[at] = l[r];
+            }
+          }
+          if (tm != tn) {  // its mirror image: four consecutive columns of row `col`
+            const int64_t at = (int64_t)col * g.ldc + row;
+            *reinterpret_cast<u32x2*>(ch + at) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+            if constexpr (PAIR)
+              *reinterpret_cast<u32x2*>(cl + at) = u32x2{l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16};
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int64_t at = (int64_t)(row + r) * g.ldc + col;
+            uint16_t h[Core::VEC], l[Core::VEC];
+#pragma unroll
+            for (int k = 0; k < Core::VEC; ++k) {
+              const float v = alpha * acc[f][i + k][4 * q + r];
+              h[k] = to_f16(v);
+              l[k] = to_f16(v - f16_to_f32(h[k]));
+            }
+            if constexpr (Core::VEC == 4) {
+              *reinterpret_cast<u32x2*>(ch + at) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+              if constexpr (PAIR)
+                *reinterpret_cast<u32x2*>(cl + at) = u32x2{l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16};
+            } else {
+              ch[at] = h[0];
+              if constexpr (PAIR) cl[at] = l[0];
+            }
+          }
+        }
+      }
+}
+
+// ---------------------------------------------------------------- elementwise passes
+// The update's direction u of one element: the momentum buffer's new value b' = mu b +
+// s g (s g at step 1), and u = s g + mu b' (Nesterov) or b'. Without a buffer u = s g.
+struct Direction {
+  float mu, s;
+  bool first, nesterov;
+  __device__ __forceinline__ float state(float g, float b) const { return first ? s * g : fmaf(mu, b, s * g); }
+  __device__ __forceinline__ float u(float g, float b1) const { return nesterov ? fmaf(mu, b1, s * g) : b1; }
+};
+
+// Pointers of a batch, by value.
+struct NsPtrs {
+  const void* x[kMaxMats];   // X, or the gradient
+  float* state[kMaxMats];
+  uint8_t id[kMaxMats];
+};
+
+struct NsEw {
+  int64_t numel;
+  int rows_n, cols_m;        // n, m
+  int np, mp;                // padded
+  uint64_t tall;
+  double eps;
+  float momentum;
+  int first, nesterov;
+  double clip_frac;          // > 0: clip the gradient against W_sumsq
+  const double* grad_sumsq;
+  const double* W_sumsq;
+  float* clip_scale;
+  double* part;              // [count][kNsNormBlocks]
+};
+
+template <bool MUON>
+__device__ __forceinline__ Direction direction(const NsEw& a, const NsPtrs& p, int mat) {
+  Direction d{};
+  if constexpr (MUON) {
+    const int id = p.id[mat];
+    d.mu = p.state[mat] ? a.momentum : 0.f;
+    d.first = a.first != 0 || !p.state[mat];
+    d.nesterov = a.nesterov != 0 && p.state[mat];
+    d.s = a.clip_frac > 0.0 ? clip_factor(a.grad_sumsq[id], a.W_sumsq[id], a.clip_frac) : 1.f;
+  }
+  return d;
+}
+
+// Momentum (MUON: the state in place) and the block's share of ||u||^2, in double.
+template <typename T, bool MUON>
+__global__ __launch_bounds__(256) void ns_norm_kernel(NsEw a, NsPtrs p) {
+  __shared__ double red[4];
+  const int mat = blockIdx.y;
+  const T* x = (const T*)p.x[mat];
+  float* st = MUON ? p.state[mat] : nullptr;
+  const Direction d = direction<MUON>(a, p, mat);
+  double sum = 0.0;
+  // every block takes an equal run of 1024-element pieces
+  const int64_t pieces = (a.numel + 1023) / 1024, per = (pieces + gridDim.x - 1) / gridDim.x;
+  const int64_t i1 = min(a.numel, (int64_t)(blockIdx.x + 1) * per * 1024);
+  for (int64_t i = (int64_t)blockIdx.x * per * 1024 + threadIdx.x * 4; i < i1; i += 1024) {
+    f32x4 v = ld4<T>(x, i);
+    if constexpr (MUON) {
+      f32x4 b = st && !d.first ? ld4<float>(st, i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        b[k] = d.state(v[k], b[k]);
+        v[k] = d.u(v[k], b[k]);
+      }
+      if (st) st4<float>(st, i, b);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum = fma((double)v[k], (double)v[k], sum);
+  }
+  sum = block_sum_d(sum, red);
+  if (threadIdx.x == 0) {
+    a.part[(int64_t)mat * kNsNormBlocks + blockIdx.x] = sum;
+    if (MUON && blockIdx.x == 0 && a.clip_scale) a.clip_scale[p.id[mat]] = d.s;
+  }
+}
+
+// X = 2^e u / (||u|| + eps) as fp16 hi + lo, n x m and padded with zeros; one 64 x 64
+// tile a workgroup. A tall matrix is transposed through LDS.
+template <typename T, bool MUON>
+__global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat X, float pow2, int nblk) {
+  __shared__ float tile[kNsEdge][kNsEdge + 1];
+  __shared__ double red[4];
+  const int mat = blockIdx.z, t = threadIdx.x;
+  const int i0 = blockIdx.y * kNsEdge, j0 = blockIdx.x * kNsEdge;  // rows and columns of X
+  const double* part = a.part + (int64_t)mat * kNsNormBlocks;
+  double s = 0.0;
+  for (int k = t; k < nblk; k += 256) s += part[k];
+  s = sqrt(block_sum_d(s, red)) + a.eps;
+  const float f = s == 0.0 ? 0.f : (float)(pow2 / s);
+  const T* x = (const T*)p.x[mat];
+  const float* st = MUON ? p.state[mat] : nullptr;
+  const Direction d = direction<MUON>(a, p, mat);
+  const bool tall = (a.tall >> mat) & 1;
+  // source rows and columns of this tile
+  const int R = tall ? a.cols_m : a.rows_n, C = tall ? a.rows_n : a.cols_m;
+  const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+  uint16_t* hi = X.hi + mat * X.stride;
+  uint16_t* lo = X.lo + mat * X.stride;
+  auto put = [&](int i, int j, f32x4 v) {
+    u32x2 h, l;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint16_t h0 = to_f16(v[2 * k]), h1 = to_f16(v[2 * k + 1]);
+      h[k] = h0 | (uint32_t)h1 << 16;
+      l[k] = to_f16(v[2 * k] - f16_to_f32(h0)) | (uint32_t)to_f16(v[2 * k + 1] - f16_to_f32(h1)) << 16;
+    }
+    const int64_t at = (int64_t)i * a.mp + j;
+    *reinterpret_cast<u32x2*>(hi + at) = h;
+    *reinterpret_cast<u32x2*>(lo + at) = l;
+  };
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 16 + (t >> 4), c = 4 * (t & 15);
+    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (r0 + r < R && c0 + c < C) {  // C is a multiple of 8
+      const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
+      v = ld4<T>(x, at);
+      if constexpr (MUON) {
+        const f32x4 b = st ? ld4<float>(st, at) : v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = st ? d.u(v[q], b[q]) : d.s * v[q];
+      }
+      v *= f;
+    }
+    if (!tall) {
+      put(i0 + r, j0 + c, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tile[r][c + q] = v[q];
+    }
+  }
+  if (!tall) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int i = k * 16 + (t >> 4), j = 4 * (t & 15);
+    put(i0 + i, j0 + j, f32x4{tile[j][i], tile[j + 1][i], tile[j + 2][i], tile[j + 3][i]});
+  }
+}
+
+// Four consecutive entries (r, c..c+3) of the result in the caller's orientation, from X
+// (n x m) or, for a tall matrix, X^T: tile by tile through LDS.
+template <bool PAIR>
+struct XTile {
+  float (*tile)[kNsEdge + 1];
+  __device__ __forceinline__ f32x4 load(const uint16_t* hi, const uint16_t* lo, int64_t at) const {
+    const f16x4 h = *reinterpret_cast<const f16x4*>(hi + at);
+    f32x4 v = {(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
+    if constexpr (PAIR) {
+      const f16x4 l = *reinterpret_cast<const f16x4*>(lo + at);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += (float)l[k];
+    }
+    return v;
+  }
+};
+
+struct NsFinish {
+  int R[2], C[2];            // rows and columns of the caller's matrix: [0] wide, [1] tall
+  int mp;
+  uint64_t tall;
+  float pow2;                // 2^-e of X
+  int lp_bf16;
+  // muon
+  float decay, lr_wd;        // 1 - lr weight_decay, lr weight_decay
+  float step[2];             // lr times the scale of O, by orientation
+  int clip_update;
+  double clip_frac;
+  double* W_sumsq;
+  float* clip_scale;
+  double* part;              // [count][tiles]
+  double* dsq;               // [count] ||delta||^2
+};
+struct NsOutPtrs {
+  float* W[kMaxMats];
+  void* o[kMaxMats];         // O, or the low-precision copy of W
+  uint8_t id[kMaxMats];
+};
+
+enum { kWriteO = 0, kApply = 1, kDelta = 2 };
+
+// One 64 x 64 tile of the caller's matrix: O = X 2^-e written (kWriteO); the step on W,
+// W' = decay W - step O (kApply), or with the update clipped W' = W + k delta, delta =
+// -lr_wd W - step O; or the tile's share of ||delta||^2 (kDelta).
+template <typename T, int WHAT, bool PAIR>
+__global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p, NsMat X) {
+  __shared__ float tile[kNsEdge][kNsEdge + 1];
+  __shared__ double red[4];
+  const int mat = blockIdx.z, t = threadIdx.x;
+  const bool tall = (a.tall >> mat) & 1;
+  const int i0 = blockIdx.y * kNsEdge, j0 = blockIdx.x * kNsEdge;  // of X
+  const int R = a.R[tall], C = a.C[tall];
+  const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+  const uint16_t* hi = X.hi + mat * X.stride;
+  const uint16_t* lo = PAIR ? X.lo + mat * X.stride : nullptr;
+  const XTile<PAIR> xt{tile};
+  if (tall) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = k * 16 + (t >> 4), j = 4 * (t & 15);
+      const f32x4 v = xt.load(hi, lo, (int64_t)(i0 + i) * a.mp + j0 + j);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tile[j + q][i] = v[q];
+    }
+    __syncthreads();
+  }
+  const int id = p.id[mat];
+  const float step = a.step[tall];
+  float k_clip = 1.f;
+  if constexpr (WHAT == kApply) {
+    if (a.clip_update) k_clip = clip_factor(a.dsq[mat], a.W_sumsq[id], a.clip_frac);
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 16 + (t >> 4), c = 4 * (t & 15);
+    if (r0 + r >= R || c0 + c >= C) continue;
+    f32x4 v;
+    if (tall)
+      v = f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]};
+    else
+      v = xt.load(hi, lo, (int64_t)(i0 + r) * a.mp + j0 + c);
+    v *= a.pow2;
+    const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
+    if constexpr (WHAT == kWriteO) {
+      st4<T>((T*)p.o[mat], at, v);
+    } else {
+      f32x4 w = ld4<float>(p.W[mat], at);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float delta = fmaf(-step, v[q], -a.lr_wd * w[q]);
+        if constexpr (WHAT == kDelta)
+          sum = fma((double)delta, (double)delta, sum);
+        else
+          w[q] = a.clip_update ? fmaf(k_clip, delta, w[q]) : fmaf(-step, v[q], a.decay * w[q]);
+      }
+      if constexpr (WHAT == kApply) {
+        st4<float>(p.W[mat], at, w);
+        if (p.o[mat]) st4<T>((T*)p.o[mat], at, w);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum = fma((double)w[q], (double)w[q], sum);
+      }
+    }
+  }
+  if constexpr (WHAT != kWriteO) {
+    sum = block_sum_d(sum, red);
+    if (t == 0) {
+      a.part[((int64_t)mat * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x] = sum;
+      if (WHAT == kApply && a.clip_update && a.clip_scale && blockIdx.x == 0 && blockIdx.y == 0)
+        a.clip_scale[id] = k_clip;
+    }
+  }
+}
+
+// Per-matrix sums of the tiles' partials: into dsq, or W_sumsq of the caller's index.
+__global__ __launch_bounds__(256) void ns_reduce_kernel(const double* part, int64_t tiles, double* dsq,
+                                                        double* W_sumsq, NsOutPtrs p) {
+  __shared__ double red[4];
+  const int mat = blockIdx.x;
+  const double s = block_sum_d(strided_sum_d(part + mat * tiles, 0, tiles), red);
+  if (threadIdx.x == 0) {
+    if (dsq)
+      dsq[mat] = s;
+    else
+      W_sumsq[p.id[mat]] = s;
+  }
+}
+
+// ---------------------------------------------------------------- workspace
+constexpr int64_t kNsAlign = 256;
+
+struct NsSpace {
+  NsMat Xa, Xb;      // n x m: the iterates in turn
+  NsMat A, C, P[3];  // n x n: Gram matrix, B A, and three for B and the product of the B
+  double* norm_part;
+  double* part;
+  double* dsq;
+  size_t bytes;
+};
+
+NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
+  char* base = (char*)ws;
+  size_t off = 0;
+  auto take = [&](int64_t bytes) {
+    char* p = base ? base + off : nullptr;
+    off += (size_t)(ceil_div(bytes, kNsAlign) * kNsAlign);
+    return p;
+  };
+  const int64_t np = ns_pad(n), mp = ns_pad(m);
+  auto mat = [&](int64_t elems, bool pair) {
+    NsMat x{};
+    x.stride = elems;
+    x.hi = (uint16_t*)take(2 * elems * count);
+    if (pair) x.lo = (uint16_t*)take(2 * elems * count);
+    return x;
+  };
+  NsSpace s{};
+  s.Xa = mat(np * mp, true);  // the first X is a pair with either type
+  s.Xb = mat(np * mp, !bf16);
+  s.A = mat(np * np, !bf16);
+  s.C = mat(np * np, !bf16);
+  for (auto& q : s.P) q = mat(np * np, !bf16);
+  s.norm_part = (double*)take(8 * (int64_t)count * kNsNormBlocks);
+  s.part = (double*)take(8 * (int64_t)count * (np / kNsEdge) * (mp / kNsEdge));
+  s.dsq = (double*)take(8 * (int64_t)count);
+  s.bytes = off;
+  return s;
+}
+
+#define FPO_CHECK_LAUNCH()             \
+  do {                                 \
+    hipError_t e_ = hipGetLastError(); \
+    if (e_ != hipSuccess) return e_;   \
+  } while (0)
+
+template <int EDGE, bool FAST, bool SYM, int EPI, bool PAIR>
+void launch_gemm(const char* name, NsGemmArgs g, int sets, hipStream_t st) {
+  const int64_t ntm = ceil_div(g.M, EDGE), ntn = ceil_div(g.N, EDGE);
+  g.tiles = (int)(SYM ? ntm * (ntm + 1) / 2 : ntm * ntn);
+  FPO_LAUNCH(name, st,
+             (ns_gemm_kernel<EDGE, FAST, SYM, EPI, PAIR><<<dim3((unsigned)(g.tiles * g.count * sets)), dim3(256), 0,
+                                                           st>>>(g)));
+}
+
+template <bool SYM, int EPI, bool PAIR>
+void launch_gemm_any(const char* name, const NsGemmArgs& g, int sets, hipStream_t st) {
+  launch_gemm<128, false, SYM, EPI, PAIR>(name, g, sets, st);
+}
+
+template <typename T, bool PAIR>
+hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
+  hipStream_t st = (hipStream_t)a.stream;
+  const int64_t n = b.n, m = b.m, np = ns_pad(n), mp = ns_pad(m);
+  const NsSpace s = ns_carve(n, m, b.count, a.bf16, a.ws);
+  const NsPlan pl = ns_plan(a.steps, a.coef, ns_three_first(n, m, a.bf16));
+  NsPtrs p{};
+  NsOutPtrs o{};
+  for (int i = 0; i < b.count; ++i) {
+    p.x[i] = a.muon ? (const void*)b.grad[i] : b.x[i];
+    p.state[i] = b.state[i];
+    p.id[i] = o.id[i] = (uint8_t)b.id[i];
+    o.W[i] = b.W[i];
+    o.o[i] = a.muon ? b.W_lp[i] : b.o[i];
+  }
+  NsEw e{};
+  e.numel = n * m;
+  e.rows_n = (int)n;
+  e.cols_m = (int)m;
+  e.np = (int)np;
+  e.mp = (int)mp;
+  e.tall = b.tall;
+  e.eps = a.eps;
+  e.momentum = a.momentum;
+  e.first = a.first;
+  e.nesterov = a.nesterov;
+  e.clip_frac = a.clip_update ? 0.0 : a.clip_frac;
+  e.grad_sumsq = a.grad_sumsq;
+  e.W_sumsq = a.W_sumsq;
+  e.clip_scale = a.clip_update ? nullptr : a.clip_scale;
+  e.part = s.norm_part;
+  const int nblk = (int)std::min<int64_t>(kNsNormBlocks, ceil_div(n * m, 4096));
+  const dim3 tiles((unsigned)(mp / kNsEdge), (unsigned)(np / kNsEdge), (unsigned)b.count);
+  const float pow_in = (float)std::ldexp(1.0, pl.groups[0].e_X);
+  if (a.muon) {
+    FPO_LAUNCH("muon_momentum", st,
+               (ns_norm_kernel<float, true><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
+    FPO_CHECK_LAUNCH();
+    FPO_LAUNCH("ns_convert", st,
+               (ns_convert_kernel<float, true><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+  } else {
+    FPO_LAUNCH("ns_norm", st, (ns_norm_kernel<T, false><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
+    FPO_CHECK_LAUNCH();
+    FPO_LAUNCH("ns_convert", st,
+               (ns_convert_kernel<T, false><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+  }
+  FPO_CHECK_LAUNCH();
+
+  NsMat X = s.Xa, Y = s.Xb;
+  const auto sq = [&](const NsMat& l, const NsMat& r, const NsMat& out, double alpha) {
+    NsGemmArgs g{};
+    g.a[0] = l;
+    g.b[0] = r;
+    g.c[0] = out;
+    g.lda = g.ldb = g.ldc = (int)np;
+    g.M = g.N = g.K = (int)np;
+    g.count = b.count;
+    g.nseg = PAIR ? 3 : 1;
+    g.alpha[0] = (float)alpha;
+    return g;
+  };
+  for (int gi = 0; gi < pl.ngroups; ++gi) {
+    const NsGroup& gr = pl.groups[gi];
+    const NsStep* sp = &pl.steps[gr.first];
+    {  // A = X X^T
+      NsGemmArgs g = sq(X, X, s.A, std::ldexp(1.0, sp[0].e_A - 2 * gr.e_X));
+      g.lda = g.ldb = (int)mp;
+      g.K = (int)mp;
+      launch_gemm_any<true, kScale, PAIR>("ns_gram", g, 1, st);
+      FPO_CHECK_LAUNCH();
+    }
+    // P[q]: the product of the B so far; the other two are free
+    int q = 0;
+    for (int j = 0; j < gr.count; ++j) {
+      const int bj = j ? (q + 1) % 3 : 0;  // where B_j goes
+      {
+        NsGemmArgs g = sq(s.A, s.A, s.P[bj], sp[j].c * std::ldexp(1.0, sp[j].e_B - 2 * sp[j].e_A));
+        g.e = s.A;
+        g.beta = (float)(sp[j].b * std::ldexp(1.0, sp[j].e_B - sp[j].e_A));
+        g.diag = (float)(sp[j].a * std::ldexp(1.0, sp[j].e_B));
+        launch_gemm_any<true, kPoly, PAIR>("ns_poly", g, 1, st);
+        FPO_CHECK_LAUNCH();
+      }
+      // the product of the B, and B A on the way to the next A = B A B, in one launch
+      const bool more = j + 1 < gr.count;
+      const int qn = j ? (q + 2) % 3 : 0;
+      if (j || more) {
+        NsGemmArgs g{};
+        int sets = 0;
+        float al[2];
+        auto add = [&](const NsMat& l, const NsMat& r, const NsMat& out, int shift) {
+          const NsGemmArgs one = sq(l, r, out, 1.0);
+          if (!sets) g = one;
+          g.a[sets] = l;
+          g.b[sets] = r;
+          g.c[sets] = out;
+          al[sets++] = (float)std::ldexp(1.0, shift);
+        };
+        if (j) add(s.P[bj], s.P[q], s.P[qn], sp[j].e_Q - sp[j].e_B - sp[j - 1].e_Q);
+        if (more) add(s.P[bj], s.A, s.C, sp[j].e_C - sp[j].e_B - sp[j].e_A);
+        for (int k = 0; k < sets; ++k) g.alpha[k] = al[k];
+        launch_gemm_any<true, kScale, PAIR>("ns_mul", g, sets, st);
+        FPO_CHECK_LAUNCH();
+      }
+      if (more) {
+        launch_gemm_any<true, kScale, PAIR>(
+            "ns_mul", sq(s.C, s.P[bj], s.A, std::ldexp(1.0, sp[j + 1].e_A - sp[j].e_C - sp[j].e_B)), 1, st);
+        FPO_CHECK_LAUNCH();
+      }
+      q = qn;
+    }
+    // X <- Q X
+    const int e_next = gi + 1 < pl.ngroups ? pl.groups[gi + 1].e_X : pl.e_out;
+    NsGemmArgs g = sq(s.P[q], X, Y, std::ldexp(1.0, e_next - gr.e_X - sp[gr.count - 1].e_Q));
+    g.ldb = g.ldc = (int)mp;
+    g.N = (int)mp;
+    g.nseg = PAIR ? 3 : gi == 0 ? 2 : 1;
+    launch_gemm_any<false, kScale, PAIR>("ns_apply", g, 1, st);
+    FPO_CHECK_LAUNCH();
+    std::swap(X, Y);
+  }
+
+  NsFinish f{};
+  f.R[0] = f.C[1] = (int)n;
+  f.C[0] = f.R[1] = (int)m;
+  f.mp = (int)mp;
+  f.tall = b.tall;
+  f.pow2 = (float)std::ldexp(1.0, -pl.e_out);
+  f.part = s.part;
+  f.dsq = s.dsq;
+  if (!a.muon) {
+    FPO_LAUNCH("ns_write", st, (ns_finish_kernel<T, kWriteO, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
+    FPO_CHECK_LAUNCH();
+    return hipSuccess;
+  }
+  const auto scale = [&](double rows, double cols) {
+    return a.scale == kNsScaleRms        ? 0.2 * std::sqrt(std::max(rows, cols))
+           : a.scale == kNsScaleSpectral ? std::sqrt(std::max(1.0, rows / cols))
+                                         : 1.0;
+  };
+  f.step[0] = (float)(a.lr * scale((double)n, (double)m));
+  f.step[1] = (float)(a.lr * scale((double)m, (double)n));
+  f.decay = (float)(1.0 - a.lr * a.weight_decay);
+  f.lr_wd = (float)(a.lr * a.weight_decay);
+  f.clip_update = a.clip_update;
+  f.clip_frac = a.clip_frac;
+  f.W_sumsq = a.W_sumsq;
+  f.clip_scale = a.clip_scale;
+  const int64_t ntiles = (np / kNsEdge) * (mp / kNsEdge);
+  if (a.clip_update) {
+    FPO_LAUNCH("muon_delta", st, (ns_finish_kernel<T, kDelta, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
+    FPO_CHECK_LAUNCH();
+    FPO_LAUNCH("muon_reduce", st,
+               ns_reduce_kernel<<<dim3(b.count), dim3(256), 0, st>>>(s.part, ntiles, s.dsq, nullptr, o));
+    FPO_CHECK_LAUNCH();
+  }
+  FPO_LAUNCH("muon_apply", st, (ns_finish_kernel<T, kApply, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
+  FPO_CHECK_LAUNCH();
+  if (a.W_sumsq) {
+    FPO_LAUNCH("muon_reduce", st,
+               ns_reduce_kernel<<<dim3(b.count), dim3(256), 0, st>>>(s.part, ntiles, nullptr, a.W_sumsq, o));
+    FPO_CHECK_LAUNCH();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t ns_workspace(int64_t n, int64_t m, int count, bool bf16) { return ns_carve(n, m, count, bf16, nullptr).bytes; }
+
+hipError_t launch_ns(const NsLaunch& a, const NsBatch& b) {
+  return a.bf16 ? run_ns<uint16_t, false>(a, b) : run_ns<float, true>(a, b);
+}
+
+}  // namespace fpo

@@ -316,4 +316,26 @@ struct CosLaunch {
 hipError_t launch_cosine(const CosLaunch& a);
 int64_t cosine_blocks(int64_t numel);
 
+struct LnLaunch {
+  bool bf16, dy_bf16;
+  int64_t T, d;
+  float eps, min_std;
+  const void* x;
+  const void* gain;   // null: ones
+  const void* bias;   // null: zeros (forward)
+  void* y;
+  float* mean;
+  float* rstd;
+  const void* dy;
+  float* dx;
+  void* dx_lp;
+  float* dgain;
+  float* dbias;
+  float* part;        // [2][blocks][d] when there are several blocks
+  void* stream;
+};
+hipError_t launch_layernorm(const LnLaunch& a);
+hipError_t launch_layernorm_vjp(const LnLaunch& a);
+int ln_vjp_blocks(int64_t T, int64_t d);
+
 }  // namespace fpo

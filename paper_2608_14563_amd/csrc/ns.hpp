@@ -1,0 +1,198 @@
+// Orthogonalisation by Newton-Schulz products (host side): how the steps are
+// grouped into products, the power of two each matrix is stored with, and the
+// launch description of fpo_orthogonalize and fpo_muon_update.
+#pragma once
+
+#include <stdint.h>
+
+#include <cmath>
+#include <algorithm>
+
+#include "launch.hpp"
+
+namespace fpo {
+
+constexpr int kNsMaxSteps = 32;
+
+// One step maps every singular value s of X to p(s) = a s + b s^3 + c s^5, that is
+// X' = B X with B = a I + b A + c A^2 and A = X X^T (n x n, n the shorter side).
+struct NsStep {
+  double a, b, c;
+  double r_in;      // bound of X's largest singular value before the step (X starts with Frobenius norm <= 1)
+  double r_out;     // and after it
+  double b_max;     // bound of B's largest eigenvalue magnitude
+  int e_A, e_B, e_C, e_Q;  // stored as 2^e times the value: A, B, B A, the group's product of the B
+};
+
+// Steps [first, first + count) of one group: all their B are formed from A by n x n
+// products (the next A is B A B), and X is multiplied once, by the product of the B.
+struct NsGroup {
+  int first, count;
+  int e_X;  // exponent of the X that the group reads
+};
+
+struct NsPlan {
+  int nsteps = 0, ngroups = 0;
+  NsStep steps[kNsMaxSteps];
+  NsGroup groups[kNsMaxSteps];
+  int e_out = 0;     // exponent of the last X
+  bool ok = false;   // false: the coefficients let X grow without bound
+};
+
+// Exponent for values of magnitude up to `bound`: 2^13 at most, an eighth of fp16's
+// largest, so that rounding errors that a step enlarges have room too.
+inline int ns_exponent(double bound) {
+  int e = 0;
+  std::frexp(bound > 1e-30 ? bound : 1e-30, &e);  // bound < 2^e
+  const int r = 13 - e;
+  return r > 40 ? 40 : r;
+}
+
+// Largest |a + b l + c l^2| over l in [0, top].
+inline double ns_poly_max(double a, double b, double c, double top) {
+  auto f = [&](double l) { return std::fabs(a + b * l + c * l * l); };
+  double m = f(0.0) > f(top) ? f(0.0) : f(top);
+  if (c != 0.0) {
+    const double v = -b / (2 * c);
+    if (v > 0.0 && v < top && f(v) > m) m = f(v);
+  }
+  return m;
+}
+
+// Largest |p(s)| over s in [0, top]: at the end or where p' = a + 3 b u + 5 c u^2 = 0, u = s^2.
+inline double ns_value_max(double a, double b, double c, double top) {
+  auto f = [&](double s) { return std::fabs(s * (a + b * s * s + c * s * s * s * s)); };
+  double m = f(top);
+  auto at = [&](double u) {
+    if (u > 0.0 && u < top * top && f(std::sqrt(u)) > m) m = f(std::sqrt(u));
+  };
+  if (c != 0.0) {
+    const double d = 9 * b * b - 20 * a * c;
+    if (d >= 0.0) {
+      at((-3 * b + std::sqrt(d)) / (10 * c));
+      at((-3 * b - std::sqrt(d)) / (10 * c));
+    }
+  } else if (b != 0.0) {
+    at(-a / (3 * b));
+  }
+  return m;
+}
+
+// Groups. With g steps in a group and r = m / n a group costs, in n x n x n half
+// products, 3 r + 1 + 4 (g - 1): longer groups are cheaper, the more the wider X is.
+// What limits them is rounding: A is rounded once a group, and B A B carries that error
+// on, enlarged by up to b_max^2 a step, while X's small singular values rely on A's
+// small eigenvalues. Relative error of five steps of (3.4445, -4.775, 2.0315) against
+// 64 bits with fp16 products, groups 3+2 / 2+1+2 / one step each / 2+3 (emulated):
+// normal entries 256 x 768 1.7e-3 / 1.0e-3 / 1.1e-3 / 1.0e-3, 264 x 264 1.7e-3 / 1.4e-3
+// / 1.2e-3 / 4.0e-3, 8 x 8 4.5e-3 / 1.5e-3 / 1.0e-3 / 1.4e-3; singular values 1/k 3.3e-3 /
+// 1.3e-3 / 1.5e-3 / 4.5e-3; rank 34 of 136 4.7e-3 / 1.0e-2 / 1.9e-2 / 1.7e-2; all five
+// together overflow. So with fp16 products the first group takes three steps where that
+// is cheaper by more than 7% (r >= 1.5, where also the singular values of a matrix of
+// full rank keep away from zero); otherwise, and with pairs, whose point is accuracy,
+// two steps a group and the odd one second. Coefficients that enlarge more close a
+// group earlier (kNsGrowth is a little over 3.4445^4).
+constexpr double kNsGrowth = 150.0;
+constexpr double kNsMaxSigma = 1024.0;
+
+inline bool ns_three_first(int64_t n, int64_t m, bool bf16) { return bf16 && 2 * m >= 3 * n; }
+
+inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
+  static const double kDefault[3] = {3.4445, -4.7750, 2.0315};
+  NsPlan p;
+  double r = 1.0;
+  for (int i = 0; i < steps; ++i) {
+    const double* k = coef ? coef + 3 * i : kDefault;
+    NsStep s{};
+    s.a = k[0];
+    s.b = k[1];
+    s.c = k[2];
+    s.r_in = r;
+    s.b_max = ns_poly_max(s.a, s.b, s.c, r * r);
+    r = ns_value_max(s.a, s.b, s.c, r);
+    s.r_out = r;
+    if (!(r <= kNsMaxSigma) || !(s.b_max <= kNsMaxSigma * kNsMaxSigma)) return p;
+    p.steps[p.nsteps++] = s;
+  }
+  for (int i = 0; i < steps;) {
+    const bool odd = steps % 2 == 1;
+    const int longest = odd && three_first && i == 0 ? 3 : odd && !three_first && p.ngroups == 1 ? 1 : 2;
+    NsGroup g{i, 1, ns_exponent(p.steps[i].r_in)};
+    double growth = p.steps[i].b_max * p.steps[i].b_max, q = p.steps[i].b_max;
+    while (g.count < longest && i + g.count < steps && growth <= kNsGrowth) {
+      const double b = p.steps[i + g.count].b_max;
+      growth *= b * b;
+      ++g.count;
+    }
+    for (int j = 0; j < g.count; ++j) {
+      NsStep& s = p.steps[i + j];
+      if (j) q *= s.b_max;
+      s.e_A = ns_exponent(s.r_in * s.r_in);
+      s.e_B = ns_exponent(s.b_max);
+      s.e_C = ns_exponent(s.b_max * s.r_in * s.r_in);
+      s.e_Q = j ? ns_exponent(q) : s.e_B;
+    }
+    p.groups[p.ngroups++] = g;
+    i += g.count;
+  }
+  p.e_out = ns_exponent(r);
+  p.ok = true;
+  return p;
+}
+
+// ---------------------------------------------------------------- launch
+constexpr int kNsNormBlocks = 512;   // workgroups (and partials) a matrix of the norm pass
+constexpr int kNsEdge = 64;          // edge of the tiles of the elementwise passes; n and m are padded to it
+
+inline int64_t ns_pad(int64_t v) { return ceil_div(v, kNsEdge) * kNsEdge; }
+
+// The matrices of one call that share (n, m), n the shorter side: one batch of launches.
+struct NsBatch {
+  int count;
+  int64_t n, m;               // true sizes, n <= m
+  int id[kMaxMats];           // the caller's index (of the per-matrix device arrays)
+  uint64_t tall;              // bit i: matrix i has more rows than columns
+  // fpo_orthogonalize: x read (f32 or bf16), o written in the same type.
+  const void* x[kMaxMats];
+  void* o[kMaxMats];
+  // fpo_muon_update
+  const float* grad[kMaxMats];
+  float* state[kMaxMats];     // null entries: no momentum
+  float* W[kMaxMats];
+  void* W_lp[kMaxMats];
+};
+
+enum { kNsScaleNone = 0, kNsScaleSpectral = 1, kNsScaleRms = 2 };  // fpo_muon_scale
+
+struct NsLaunch {
+  int steps;
+  const double* coef;
+  bool bf16;                  // element type of x, o, W_lp; bf16: fp16 products, f32: pairs of fp16
+  double eps;
+  bool muon;
+  bool first, nesterov;
+  float momentum;
+  double clip_frac;
+  bool clip_update;
+  double lr, weight_decay;
+  int scale;                  // fpo_muon_scale
+  const double* grad_sumsq;
+  double* W_sumsq;
+  float* clip_scale;
+  void* ws;
+  void* stream;
+};
+
+// Matrices of one batch at most. A batch's smallest launches (n x n, tiles on and under
+// the diagonal) should fill the CUs several times; a larger one only costs workspace.
+inline int ns_batch_limit(int64_t n, int64_t m) {
+  const int64_t t = ceil_div(n, 256), tri = t * (t + 1) / 2;
+  const int64_t want = ceil_div(8 * kCus, tri);
+  (void)m;
+  return (int)std::min<int64_t>(kMaxMats, std::max<int64_t>(want, 4));
+}
+
+size_t ns_workspace(int64_t n, int64_t m, int count, bool bf16);
+hipError_t launch_ns(const NsLaunch& a, const NsBatch& b);
+
+}  // namespace fpo
