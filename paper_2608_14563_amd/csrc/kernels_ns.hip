@@ -12,11 +12,10 @@
 // times a power of two that keeps a bound of its spectral norm under 2^13 (ns.hpp), so
 // that fp16's range is no concern and its 11 bits count: with bf16 operands (8 bits)
 // the five-step result of a 512 x 1536 normal matrix is off by 1.1e-2 against 64 bits,
-// with fp16 by 1.3e-3. The matrix instructions run at the same rate. The first X is
-// kept as a pair hi + lo of fp16 for its product with the factors: its small singular
-// values are enlarged most (3.4445^5 = 485 times), and so is its rounding. With float32
-// operands every matrix is such a pair and a product the three hi hi + hi lo + lo hi:
-// 22 to 23 bits at three times the work, where fp32 matrix instructions take 16 times.
+// with fp16 by 1.3e-3, and half of that with what the diagonals lose to rounding kept
+// (NsMat). The matrix instructions run at the same rate. With float32 operands every
+// matrix is a pair hi + lo of fp16 and a product the three hi hi + hi lo + lo hi: 22 to
+// 23 bits at three times the work, where fp32 matrix instructions take 16 times.
 #include "gemm2s.hpp"
 #include "gemm.hpp"
 #include "ns.hpp"
@@ -27,29 +26,38 @@ namespace fpo {
 
 namespace {
 
-// A stack of equal matrices in the workspace: fp16, or pairs of fp16 (lo set).
+// A stack of equal matrices in the workspace: fp16, or pairs of fp16 (lo set). A square
+// one without lo has `diag`: what its diagonal lost to rounding, in the same units.
+// These matrices are near multiples of I, their diagonals the largest entries, so half
+// of the rounding error of fp16 is there: 512 x 1382, five steps, 1.3e-3 against 64 bits
+// without it, 6.4e-4 with it.
 struct NsMat {
   uint16_t* hi;
   uint16_t* lo;
-  int64_t stride;  // elements from one matrix to the next
+  float* diag;
+  int64_t stride;   // elements from one matrix to the next
+  int64_t dstride;  // of diag
 };
 
-// One launch of products C = A B over `count` matrices, for one or two sets of operands.
+// One launch of products C = alpha A B over `count` matrices, for one or two sets of operands.
 struct NsGemmArgs {
   NsMat a[2], b[2], c[2];
-  NsMat e;             // kPoly: A itself, for its linear term
   int lda, ldb, ldc;
   int M, N, K;         // padded sizes (multiples of 64)
   int count, tiles;    // matrices; tiles a matrix
-  int nseg;            // operand halves: 1: hi hi, 2: hi (hi + lo), 3: (hi + lo) (hi + lo) without lo lo
-  float alpha[2];      // by set: C = alpha A B,
-  float beta, diag;    // kPoly: + beta e + diag I
+  float alpha[2];      // by set
+  float beta, eye;     // kPoly: C = alpha A A + beta A + eye I
 };
 
-enum { kScale = 0, kPoly = 1 };
+// What a launch computes. kGram: X X^T, B K-contiguous ([N][K] rows); the others have B
+// N-contiguous ([K][N]). kGram, kMul and kPoly: symmetric, tiles with tn <= tm. kApply: Q X.
+enum { kGram = 0, kMul = 1, kPoly = 2, kApplyX = 3 };
 
 __device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 __device__ __forceinline__ float f16_to_f32(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+__device__ __forceinline__ u32x2 pack4(const uint16_t (&h)[4]) {
+  return u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+}
 
 // Tile (tm, tn), tn <= tm, of entry t of the lower triangle taken row by row.
 __device__ __forceinline__ void tri_tile(int t, int& tm, int& tn) {
@@ -75,12 +83,31 @@ struct NsCore<128, BNC> {
   static constexpr int FM = G2SWave<BNC>::FM, FN = G2SWave<BNC>::FN, VEC = 1;
 };
 
-// SYM: C is symmetric, B K-contiguous ([N][K]); only tiles with tn <= tm. Otherwise B
-// is N-contiguous ([K][N]). PAIR: C is stored as hi + lo.
-template <int EDGE, bool FAST, bool SYM, int EPI, bool PAIR>
+// V consecutive entries of row i.
+template <int V>
+__device__ __forceinline__ void load_f16(const uint16_t* p, float (&v)[V]) {
+  if constexpr (V == 4) {
+    const f16x4 h = *reinterpret_cast<const f16x4*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (float)h[k];
+  } else {
+    v[0] = f16_to_f32(*p);
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_f16(uint16_t* p, const uint16_t (&h)[V]) {
+  if constexpr (V == 4) *reinterpret_cast<u32x2*>(p) = pack4(h);
+  else *p = h[0];
+}
+
+// PAIR: operands and C are hi + lo, and a product is hi hi + hi lo + lo hi. Otherwise C =
+// (A + diag(a)) (B + diag(b)) = A B + (a_i B_ij + A_ij b_j) with the products of two
+// remainders left out, for square A (a) and B (b).
+template <int EDGE, bool FAST, int WHAT, bool PAIR>
 __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
-  constexpr bool BNC = !SYM;
+  constexpr bool SYM = WHAT != kApplyX, BNC = WHAT != kGram;
   using Core = NsCore<EDGE, BNC>;
+  constexpr int VEC = Core::VEC;
   __shared__ typename Core::Smem sm;
   const int ntm = (g.M + EDGE - 1) / EDGE, ntn = (g.N + EDGE - 1) / EDGE;
   int mat = blockIdx.x / g.tiles;
@@ -103,7 +130,7 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
   else
     zero_acc2s<BNC>(acc);
 #pragma unroll 1
-  for (int s = 0; s < g.nseg; ++s) {
+  for (int s = 0; s < (PAIR ? 3 : 1); ++s) {
     const uint16_t* ap = (s == 2 ? a.lo : a.hi) + mat * a.stride + (int64_t)m0 * g.lda;
     const uint16_t* bp = (s == 1 ? b.lo : b.hi) + mat * b.stride + (BNC ? (int64_t)n0 : (int64_t)n0 * g.ldb);
     const Operand A{ap, g.lda, band_bytes(g.M - m0, g.lda)};
@@ -113,68 +140,102 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
     else
       gemm2s_mainloop<BNC, true>(sm, acc, A, B, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
   }
-  // ---- epilogue
+  // ---- epilogue (the mainloop ends with a barrier: LDS is free)
   const float alpha = set ? g.alpha[1] : g.alpha[0];
   const typename Core::Map map;
   uint16_t* ch = c.hi + mat * c.stride;
   uint16_t* cl = PAIR ? c.lo + mat * c.stride : nullptr;
-  const uint16_t* eh = EPI == kPoly ? g.e.hi + mat * g.e.stride : nullptr;
-  const uint16_t* el = EPI == kPoly && PAIR ? g.e.lo + mat * g.e.stride : nullptr;
+  const uint16_t* ah = a.hi + mat * a.stride;
+  const uint16_t* bh = b.hi + mat * b.stride;
+  const uint16_t* al = PAIR ? a.lo + mat * a.stride : nullptr;
+  const float* ad = !PAIR && WHAT != kGram ? a.diag + mat * a.dstride : nullptr;
+  const float* bd = !PAIR && (WHAT == kMul || WHAT == kPoly) ? b.diag + mat * b.dstride : nullptr;
+  float* cd = !PAIR && SYM ? c.diag + mat * c.dstride : nullptr;
+  // the tile is symmetric with tile (tn, tm): off the diagonal it is stored twice, the
+  // second time transposed, by way of LDS so that whole lines are written
+  constexpr bool STAGE = SYM && EDGE == 256 && !PAIR;
+  const bool mirror = SYM && tm != tn;
+  uint16_t* lds = reinterpret_cast<uint16_t*>(&sm);
 #pragma unroll
   for (int f = 0; f < Core::FM; ++f)
 #pragma unroll
-    for (int i = 0; i < Core::FN; i += Core::VEC)
+    for (int i = 0; i < Core::FN; i += VEC)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = m0 + map.row(f, 4 * q), col = n0 + map.col(i);
-        if (row >= g.M || col >= g.N) continue;  // M and N are multiples of 64: four rows or columns are in or out
-        if constexpr (SYM) {
-          uint16_t h[4], l[4];
+        const int lr = map.row(f, 4 * q), lc = map.col(i), row = m0 + lr, col = n0 + lc;
+        if (!FAST && (row >= g.M || col >= g.N)) continue;  // M and N are multiples of 64: blocks are in or out
+        uint16_t h[4][VEC], l[4][VEC];
+        float bdv[VEC];
+        if constexpr (!PAIR && (WHAT == kMul || WHAT == kPoly)) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float v = alpha * acc[f][i][4 * q + r];
-            const int64_t at = (int64_t)(row + r) * g.ldc + col;
-            if constexpr (EPI == kPoly) {
-              float e = f16_to_f32(eh[at]);
-              if constexpr (PAIR) e += f16_to_f32(el[at]);
-              v = fmaf(g.beta, e, v);
-              if (row + r == col) v += g.diag;
-            }
-            h[r] = to_f16(v);
-            ch[at] = h[r];
+          for (int k = 0; k < VEC; ++k) bdv[k] = bd[col + k];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t at = (int64_t)(row + r) * g.ldc + col;
+          float v[VEC], x[VEC], y[VEC];
+          const float e = !PAIR && WHAT != kGram ? ad[row + r] : 0.f;
+          if constexpr (WHAT == kPoly) {
+            load_f16<VEC>(ah + at, x);
             if constexpr (PAIR) {
-              l[r] = to_f16(v - f16_to_f32(h[r]));
-              cl[at] = l[r];
-            }
-          }
-          if (tm != tn) {  // its mirror image: four consecutive columns of row `col`
-            const int64_t at = (int64_t)col * g.ldc + row;
-            *reinterpret_cast<u32x2*>(ch + at) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
-            if constexpr (PAIR)
-              *reinterpret_cast<u32x2*>(cl + at) = u32x2{l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16};
-          }
-        } else {
+              load_f16<VEC>(al + at, y);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int64_t at = (int64_t)(row + r) * g.ldc + col;
-            uint16_t h[Core::VEC], l[Core::VEC];
-#pragma unroll
-            for (int k = 0; k < Core::VEC; ++k) {
-              const float v = alpha * acc[f][i + k][4 * q + r];
-              h[k] = to_f16(v);
-              l[k] = to_f16(v - f16_to_f32(h[k]));
+              for (int k = 0; k < VEC; ++k) x[k] += y[k];
             }
-            if constexpr (Core::VEC == 4) {
-              *reinterpret_cast<u32x2*>(ch + at) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
-              if constexpr (PAIR)
-                *reinterpret_cast<u32x2*>(cl + at) = u32x2{l[0] | (uint32_t)l[1] << 16, l[2] | (uint32_t)l[3] << 16};
+          } else if constexpr (!PAIR && WHAT == kMul) {
+            load_f16<VEC>(ah + at, x);
+            load_f16<VEC>(bh + at, y);
+          } else if constexpr (!PAIR && WHAT == kApplyX) {
+            load_f16<VEC>(bh + at, y);
+          }
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            float t = acc[f][i + k][4 * q + r];
+            if constexpr (!PAIR && WHAT == kPoly) t = fmaf(e + bdv[k], x[k], t);
+            if constexpr (!PAIR && WHAT == kMul) t = fmaf(e, y[k], fmaf(bdv[k], x[k], t));
+            if constexpr (!PAIR && WHAT == kApplyX) t = fmaf(e, y[k], t);
+            t *= alpha;
+            const bool on = SYM && row + r == col + k;
+            if constexpr (WHAT == kPoly) {
+              t = fmaf(g.beta, x[k], t);
+              if (on) t += fmaf(g.beta, e, g.eye);
+            }
+            v[k] = t;
+            h[r][k] = to_f16(t);
+            const float rest = t - f16_to_f32(h[r][k]);
+            if constexpr (PAIR) l[r][k] = to_f16(rest);
+            if (!PAIR && on) cd[col + k] = rest;
+          }
+          store_f16<VEC>(ch + at, h[r]);
+          if constexpr (PAIR) store_f16<VEC>(cl + at, l[r]);
+        }
+        if (SYM && mirror) {
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            const uint16_t ht[4] = {h[0][k], h[1][k], h[2][k], h[3][k]};
+            if constexpr (STAGE) {
+              const int cc = lc + k;
+              store_f16<4>(lds + cc * 256 + (((lr >> 3) ^ (BNC ? (cc >> 2) & 31 : cc & 31)) * 8 + (lr & 7)), ht);
             } else {
-              ch[at] = h[0];
-              if constexpr (PAIR) cl[at] = l[0];
+              const int64_t at = (int64_t)(col + k) * g.ldc + row;
+              store_f16<4>(ch + at, ht);
+              if constexpr (PAIR) {
+                const uint16_t lt[4] = {l[0][k], l[1][k], l[2][k], l[3][k]};
+                store_f16<4>(cl + at, lt);
+              }
             }
           }
         }
       }
+  if constexpr (STAGE) {
+    if (!mirror) return;
+    __syncthreads();
+    const int p = threadIdx.x & 31;
+    for (int cc = threadIdx.x >> 5; cc < 256; cc += 8)
+      if (FAST || (n0 + cc < g.N && m0 + 8 * p < g.M))
+        *reinterpret_cast<u32x4*>(ch + (int64_t)(n0 + cc) * g.ldc + m0 + 8 * p) =
+            *reinterpret_cast<const u32x4*>(lds + cc * 256 + (p ^ (BNC ? (cc >> 2) & 31 : cc & 31)) * 8);
+  }
 }
 
 // ---------------------------------------------------------------- elementwise passes
@@ -255,9 +316,9 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsEw a, NsPtrs p) {
   }
 }
 
-// X = 2^e u / (||u|| + eps) as fp16 hi + lo, n x m and padded with zeros; one 64 x 64
+// X = 2^e u / (||u|| + eps) as fp16 (PAIR: hi + lo), n x m and padded with zeros; one 64 x 64
 // tile a workgroup. A tall matrix is transposed through LDS.
-template <typename T, bool MUON>
+template <typename T, bool MUON, bool PAIR>
 __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat X, float pow2, int nblk) {
   __shared__ float tile[kNsEdge][kNsEdge + 1];
   __shared__ double red[4];
@@ -276,7 +337,7 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   const int R = tall ? a.cols_m : a.rows_n, C = tall ? a.rows_n : a.cols_m;
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
   uint16_t* hi = X.hi + mat * X.stride;
-  uint16_t* lo = X.lo + mat * X.stride;
+  uint16_t* lo = PAIR ? X.lo + mat * X.stride : nullptr;
   auto put = [&](int i, int j, f32x4 v) {
     u32x2 h, l;
 #pragma unroll
@@ -287,7 +348,7 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
     }
     const int64_t at = (int64_t)i * a.mp + j;
     *reinterpret_cast<u32x2*>(hi + at) = h;
-    *reinterpret_cast<u32x2*>(lo + at) = l;
+    if constexpr (PAIR) *reinterpret_cast<u32x2*>(lo + at) = l;
   };
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -468,19 +529,21 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
     return p;
   };
   const int64_t np = ns_pad(n), mp = ns_pad(m);
-  auto mat = [&](int64_t elems, bool pair) {
+  auto mat = [&](int64_t rows, int64_t cols) {
     NsMat x{};
-    x.stride = elems;
-    x.hi = (uint16_t*)take(2 * elems * count);
-    if (pair) x.lo = (uint16_t*)take(2 * elems * count);
+    x.stride = rows * cols;
+    x.dstride = rows;
+    x.hi = (uint16_t*)take(2 * x.stride * count);
+    if (!bf16) x.lo = (uint16_t*)take(2 * x.stride * count);
+    else if (rows == np && cols == np) x.diag = (float*)take(4 * np * count);
     return x;
   };
   NsSpace s{};
-  s.Xa = mat(np * mp, true);  // the first X is a pair with either type
-  s.Xb = mat(np * mp, !bf16);
-  s.A = mat(np * np, !bf16);
-  s.C = mat(np * np, !bf16);
-  for (auto& q : s.P) q = mat(np * np, !bf16);
+  s.Xa = mat(np, mp);
+  s.Xb = mat(np, mp);
+  s.A = mat(np, np);
+  s.C = mat(np, np);
+  for (auto& q : s.P) q = mat(np, np);
   s.norm_part = (double*)take(8 * (int64_t)count * kNsNormBlocks);
   s.part = (double*)take(8 * (int64_t)count * (np / kNsEdge) * (mp / kNsEdge));
   s.dsq = (double*)take(8 * (int64_t)count);
@@ -494,18 +557,25 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
     if (e_ != hipSuccess) return e_;   \
   } while (0)
 
-template <int EDGE, bool FAST, bool SYM, int EPI, bool PAIR>
+template <int EDGE, bool FAST, int WHAT, bool PAIR>
 void launch_gemm(const char* name, NsGemmArgs g, int sets, hipStream_t st) {
   const int64_t ntm = ceil_div(g.M, EDGE), ntn = ceil_div(g.N, EDGE);
-  g.tiles = (int)(SYM ? ntm * (ntm + 1) / 2 : ntm * ntn);
+  g.tiles = (int)(WHAT == kApplyX ? ntm * ntn : ntm * (ntm + 1) / 2);
   FPO_LAUNCH(name, st,
-             (ns_gemm_kernel<EDGE, FAST, SYM, EPI, PAIR><<<dim3((unsigned)(g.tiles * g.count * sets)), dim3(256), 0,
-                                                           st>>>(g)));
+             (ns_gemm_kernel<EDGE, FAST, WHAT, PAIR><<<dim3((unsigned)(g.tiles * g.count * sets)), dim3(256), 0,
+                                                       st>>>(g)));
 }
 
-template <bool SYM, int EPI, bool PAIR>
-void launch_gemm_any(const char* name, const NsGemmArgs& g, int sets, hipStream_t st) {
-  launch_gemm<128, false, SYM, EPI, PAIR>(name, g, sets, st);
+template <int WHAT, bool PAIR>
+hipError_t launch_product(const char* name, const NsGemmArgs& g, int sets, hipStream_t st) {
+  const int mats = g.count * sets;
+  if (!ns_big_tiles(g.M, g.N, (int64_t)g.K * (PAIR ? 3 : 1), mats, WHAT != kApplyX))
+    launch_gemm<128, false, WHAT, PAIR>(name, g, sets, st);
+  else if (g.M % 256 == 0 && g.N % 256 == 0)
+    launch_gemm<256, true, WHAT, PAIR>(name, g, sets, st);
+  else
+    launch_gemm<256, false, WHAT, PAIR>(name, g, sets, st);
+  return hipGetLastError();
 }
 
 template <typename T, bool PAIR>
@@ -547,17 +617,18 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
                (ns_norm_kernel<float, true><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
     FPO_CHECK_LAUNCH();
     FPO_LAUNCH("ns_convert", st,
-               (ns_convert_kernel<float, true><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+               (ns_convert_kernel<float, true, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
   } else {
     FPO_LAUNCH("ns_norm", st, (ns_norm_kernel<T, false><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
     FPO_CHECK_LAUNCH();
     FPO_LAUNCH("ns_convert", st,
-               (ns_convert_kernel<T, false><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+               (ns_convert_kernel<T, false, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
   }
   FPO_CHECK_LAUNCH();
 
   NsMat X = s.Xa, Y = s.Xb;
-  const auto sq = [&](const NsMat& l, const NsMat& r, const NsMat& out, double alpha) {
+  // C = 2^shift A B of square operands; more sets are added for the same launch
+  const auto product = [&](const NsMat& l, const NsMat& r, const NsMat& out, double alpha) {
     NsGemmArgs g{};
     g.a[0] = l;
     g.b[0] = r;
@@ -565,68 +636,52 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     g.lda = g.ldb = g.ldc = (int)np;
     g.M = g.N = g.K = (int)np;
     g.count = b.count;
-    g.nseg = PAIR ? 3 : 1;
     g.alpha[0] = (float)alpha;
     return g;
   };
+  hipError_t err;
   for (int gi = 0; gi < pl.ngroups; ++gi) {
     const NsGroup& gr = pl.groups[gi];
     const NsStep* sp = &pl.steps[gr.first];
     {  // A = X X^T
-      NsGemmArgs g = sq(X, X, s.A, std::ldexp(1.0, sp[0].e_A - 2 * gr.e_X));
+      NsGemmArgs g = product(X, X, s.A, std::ldexp(1.0, sp[0].e_A - 2 * gr.e_X));
       g.lda = g.ldb = (int)mp;
       g.K = (int)mp;
-      launch_gemm_any<true, kScale, PAIR>("ns_gram", g, 1, st);
-      FPO_CHECK_LAUNCH();
+      if ((err = launch_product<kGram, PAIR>("ns_gram", g, 1, st)) != hipSuccess) return err;
     }
-    // P[q]: the product of the B so far; the other two are free
-    int q = 0;
+    int q = 0;  // P[q]: the product of the B so far; the other two are free
     for (int j = 0; j < gr.count; ++j) {
-      const int bj = j ? (q + 1) % 3 : 0;  // where B_j goes
-      {
-        NsGemmArgs g = sq(s.A, s.A, s.P[bj], sp[j].c * std::ldexp(1.0, sp[j].e_B - 2 * sp[j].e_A));
-        g.e = s.A;
+      const int bj = j ? (q + 1) % 3 : 0, qn = j ? (q + 2) % 3 : 0;
+      {  // P[bj] = B_j = a I + b A + c A A
+        NsGemmArgs g = product(s.A, s.A, s.P[bj], sp[j].c * std::ldexp(1.0, sp[j].e_B - 2 * sp[j].e_A));
         g.beta = (float)(sp[j].b * std::ldexp(1.0, sp[j].e_B - sp[j].e_A));
-        g.diag = (float)(sp[j].a * std::ldexp(1.0, sp[j].e_B));
-        launch_gemm_any<true, kPoly, PAIR>("ns_poly", g, 1, st);
-        FPO_CHECK_LAUNCH();
+        g.eye = (float)(sp[j].a * std::ldexp(1.0, sp[j].e_B));
+        if ((err = launch_product<kPoly, PAIR>("ns_poly", g, 1, st)) != hipSuccess) return err;
       }
       // the product of the B, and B A on the way to the next A = B A B, in one launch
       const bool more = j + 1 < gr.count;
-      const int qn = j ? (q + 2) % 3 : 0;
-      if (j || more) {
-        NsGemmArgs g{};
-        int sets = 0;
-        float al[2];
-        auto add = [&](const NsMat& l, const NsMat& r, const NsMat& out, int shift) {
-          const NsGemmArgs one = sq(l, r, out, 1.0);
-          if (!sets) g = one;
-          g.a[sets] = l;
-          g.b[sets] = r;
-          g.c[sets] = out;
-          al[sets++] = (float)std::ldexp(1.0, shift);
-        };
-        if (j) add(s.P[bj], s.P[q], s.P[qn], sp[j].e_Q - sp[j].e_B - sp[j - 1].e_Q);
-        if (more) add(s.P[bj], s.A, s.C, sp[j].e_C - sp[j].e_B - sp[j].e_A);
-        for (int k = 0; k < sets; ++k) g.alpha[k] = al[k];
-        launch_gemm_any<true, kScale, PAIR>("ns_mul", g, sets, st);
-        FPO_CHECK_LAUNCH();
+      int sets = 0;
+      NsGemmArgs g = product(s.P[bj], s.A, s.C, 0.0);
+      if (more) g.alpha[sets++] = (float)std::ldexp(1.0, sp[j].e_C - sp[j].e_B - sp[j].e_A);
+      if (j) {
+        g.a[sets] = s.P[bj];
+        g.b[sets] = s.P[q];
+        g.c[sets] = s.P[qn];
+        g.alpha[sets++] = (float)std::ldexp(1.0, sp[j].e_Q - sp[j].e_B - sp[j - 1].e_Q);
       }
+      if (sets && (err = launch_product<kMul, PAIR>("ns_mul", g, sets, st)) != hipSuccess) return err;
       if (more) {
-        launch_gemm_any<true, kScale, PAIR>(
-            "ns_mul", sq(s.C, s.P[bj], s.A, std::ldexp(1.0, sp[j + 1].e_A - sp[j].e_C - sp[j].e_B)), 1, st);
-        FPO_CHECK_LAUNCH();
+        g = product(s.C, s.P[bj], s.A, std::ldexp(1.0, sp[j + 1].e_A - sp[j].e_C - sp[j].e_B));
+        if ((err = launch_product<kMul, PAIR>("ns_mul", g, 1, st)) != hipSuccess) return err;
       }
       q = qn;
     }
     // X <- Q X
     const int e_next = gi + 1 < pl.ngroups ? pl.groups[gi + 1].e_X : pl.e_out;
-    NsGemmArgs g = sq(s.P[q], X, Y, std::ldexp(1.0, e_next - gr.e_X - sp[gr.count - 1].e_Q));
+    NsGemmArgs g = product(s.P[q], X, Y, std::ldexp(1.0, e_next - gr.e_X - sp[gr.count - 1].e_Q));
     g.ldb = g.ldc = (int)mp;
     g.N = (int)mp;
-    g.nseg = PAIR ? 3 : gi == 0 ? 2 : 1;
-    launch_gemm_any<false, kScale, PAIR>("ns_apply", g, 1, st);
-    FPO_CHECK_LAUNCH();
+    if ((err = launch_product<kApplyX, PAIR>("ns_apply", g, 1, st)) != hipSuccess) return err;
     std::swap(X, Y);
   }
 

@@ -83,19 +83,20 @@ inline double ns_value_max(double a, double b, double c, double top) {
 // What limits them is rounding: A is rounded once a group, and B A B carries that error
 // on, enlarged by up to b_max^2 a step, while X's small singular values rely on A's
 // small eigenvalues. Relative error of five steps of (3.4445, -4.775, 2.0315) against
-// 64 bits with fp16 products, groups 3+2 / 2+1+2 / one step each / 2+3 (emulated):
-// normal entries 256 x 768 1.7e-3 / 1.0e-3 / 1.1e-3 / 1.0e-3, 264 x 264 1.7e-3 / 1.4e-3
-// / 1.2e-3 / 4.0e-3, 8 x 8 4.5e-3 / 1.5e-3 / 1.0e-3 / 1.4e-3; singular values 1/k 3.3e-3 /
-// 1.3e-3 / 1.5e-3 / 4.5e-3; rank 34 of 136 4.7e-3 / 1.0e-2 / 1.9e-2 / 1.7e-2; all five
-// together overflow. So with fp16 products the first group takes three steps where that
-// is cheaper by more than 7% (r >= 1.5, where also the singular values of a matrix of
-// full rank keep away from zero); otherwise, and with pairs, whose point is accuracy,
-// two steps a group and the odd one second. Coefficients that enlarge more close a
-// group earlier (kNsGrowth is a little over 3.4445^4).
+// 64 bits, fp16 with the diagonals' remainders (emulated), groups 3+2 / 2+1+2 / 2+2+1:
+// token-summed outer products 512 x 1382 6.4e-4 / 5.3e-4 / 9.4e-4, 512 x 512 1.1e-3 /
+// 1.0e-3 / 1.3e-3, 256 x 256 1.2e-3 / 9.7e-4 / 1.5e-3, 64 x 128 2.2e-3 / 7.4e-4 / 7.1e-4;
+// six steps 2+2+2, 512 x 512 1.6e-3; five in one group overflow. So with fp16 products
+// the first group takes three steps where that is cheaper by more than 7% (r >= 1.5,
+// where the singular values of a matrix of full rank also keep away from zero) and the
+// products' time is what counts (n >= 512: below, the launches' number, which is the
+// same); otherwise, and with pairs, whose point is accuracy, it takes two. After it
+// groups of one and two alternate. Coefficients that enlarge more close a group earlier
+// (kNsGrowth is a little over 3.4445^4).
 constexpr double kNsGrowth = 150.0;
 constexpr double kNsMaxSigma = 1024.0;
 
-inline bool ns_three_first(int64_t n, int64_t m, bool bf16) { return bf16 && 2 * m >= 3 * n; }
+inline bool ns_three_first(int64_t n, int64_t m, bool bf16) { return bf16 && n >= 512 && 2 * m >= 3 * n; }
 
 inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
   static const double kDefault[3] = {3.4445, -4.7750, 2.0315};
@@ -115,8 +116,7 @@ inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
     p.steps[p.nsteps++] = s;
   }
   for (int i = 0; i < steps;) {
-    const bool odd = steps % 2 == 1;
-    const int longest = odd && three_first && i == 0 ? 3 : odd && !three_first && p.ngroups == 1 ? 1 : 2;
+    const int longest = i == 0 ? (three_first ? 3 : 2) : (p.ngroups % 2 == 1) != three_first ? 1 : 2;
     NsGroup g{i, 1, ns_exponent(p.steps[i].r_in)};
     double growth = p.steps[i].b_max * p.steps[i].b_max, q = p.steps[i].b_max;
     while (g.count < longest && i + g.count < steps && growth <= kNsGrowth) {
@@ -141,6 +141,19 @@ inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
 }
 
 // ---------------------------------------------------------------- launch
+// Whether a launch of `mats` M x N products over K (symmetric: the tiles on and under the
+// diagonal) takes 256 x 256 tiles or 128 x 128 ones, by the estimates of big_tiles.
+inline bool ns_big_tiles(int64_t M, int64_t N, int64_t K, int64_t mats, bool symmetric) {
+  const double kt = (double)ceil_div(K, 64);
+  auto tiles = [&](int64_t edge) {
+    const int64_t tm = ceil_div(M, edge), tn = ceil_div(N, edge);
+    return mats * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
+  };
+  const int64_t big = tiles(256), rem = big % kCus;
+  const double us = (double)(big / kCus) * (1.6 * kt + 14.0) + (rem ? (1.0 + 0.6 * (double)rem / kCus) * kt + 14.0 : 0.0);
+  return us <= (double)ceil_div(tiles(128), kCus) * (0.55 * kt + 7.5);
+}
+
 constexpr int kNsNormBlocks = 512;   // workgroups (and partials) a matrix of the norm pass
 constexpr int kNsEdge = 64;          // edge of the tiles of the elementwise passes; n and m are padded to it
 
