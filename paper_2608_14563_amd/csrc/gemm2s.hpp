@@ -70,6 +70,13 @@ struct AccMap2S {
   __device__ __forceinline__ int col(int i) const { return colb + 32 * i + lc; }
 };
 
+// K tiles in three passes over the operands: (hi, hi), (hi, lo), (lo, hi), `len` each; lo
+// lies a_lo, b_lo bytes after hi. len 0: one pass.
+struct K3 {
+  int len;
+  uint32_t a_lo, b_lo;
+};
+
 template <bool BNC>
 struct Pipe2S {
   using W = G2SWave<BNC>;
@@ -172,17 +179,33 @@ __device__ __forceinline__ void read_step(Frags2S<BNC>& fr, const Pipe2S<BNC>& p
 template <bool BNC, bool F16 = false>
 __device__ __forceinline__ void gemm2s_mainloop(G2SSmem& sm, f32x16 (&acc)[G2SWave<BNC>::FM][G2SWave<BNC>::FN],
                                                 const Operand& A, const Operand& B, int M_rem, int N_rem, int K,
-                                                int kt0, int kt1) {
+                                                int kt0, int kt1, K3 k3 = K3{0, 0u, 0u}) {
   using W = G2SWave<BNC>;
   constexpr uint32_t kStage = G2S::STAGE_CHUNKS * 16;
   const int n = kt1 - kt0;
   if (n <= 0) return;
   Pipe2S<BNC> p;
   p.setup(sm.s, A, B, M_rem, N_rem, kt0);
+  // after the copies of a pass's last K tile: on to the next pass (k3.len 0: none)
+  int left = k3.len, pass = 0;
+  auto next_pass = [&] {
+    if (--left) return;
+    left = k3.len;
+    const uint32_t back_a = (uint32_t)k3.len * (G2S::BK * 2), back_b = (uint32_t)k3.len * p.stepB;
+    const uint32_t da = pass == 1 ? k3.a_lo : 0u, db = pass == 0 ? k3.b_lo : pass == 1 ? 0u - k3.b_lo : 0u;
+    ++pass;
 #pragma unroll
-  for (int t = 0; t < G2S::NST; ++t)
+    for (int q = 0; q < 4; ++q) {
+      p.offA[q] += da - back_a;
+      p.offB[q] += db - back_b;
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < G2S::NST; ++t) {
 #pragma unroll
     for (int q = 0; q < G2S::COPIES; ++q) p.issue(t, q);
+    if (k3.len) next_pass();
+  }
   Frags2S<BNC> f0, f1;
   wait_vmcnt<3 * G2S::COPIES>();
   stage_barrier();
@@ -220,6 +243,7 @@ __device__ __forceinline__ void gemm2s_mainloop(G2SSmem& sm, f32x16 (&acc)[G2SWa
         acc[f][i] = mfma_16bit<F16>(cur.a[h][f], cur.b[h][i], acc[f][i]);
         __builtin_amdgcn_sched_barrier(0);
       }
+    if (k3.len) next_pass();
   };
   int j = 0;
   for (; j + 1 < n; j += 2) {

@@ -26,15 +26,15 @@ namespace fpo {
 
 namespace {
 
-// A stack of equal matrices in the workspace: fp16, or pairs of fp16 (lo set). A square
-// one without lo has `diag`: what its diagonal lost to rounding, in the same units.
+// A stack of equal matrices in the workspace: fp16, or pairs of fp16. A square one of
+// single fp16 has `diag`: what its diagonal lost to rounding, in the same units.
 // These matrices are near multiples of I, their diagonals the largest entries, so half
 // of the rounding error of fp16 is there: 512 x 1382, five steps, 1.3e-3 against 64 bits
 // without it, 6.4e-4 with it.
 struct NsMat {
   uint16_t* hi;
-  uint16_t* lo;
   float* diag;
+  int64_t lo_off;   // elements from a hi to its lo (which follow each other)
   int64_t stride;   // elements from one matrix to the next
   int64_t dstride;  // of diag
 };
@@ -45,6 +45,7 @@ struct NsGemmArgs {
   int lda, ldb, ldc;
   int M, N, K;         // padded sizes (multiples of 64)
   int count, tiles;    // matrices; tiles a matrix
+  int nbig;            // 128 x 128 launch: the 256 x 256 tiles before it (0: all tiles are 128 x 128)
   float alpha[2];      // by set
   float beta, eye;     // kPoly: C = alpha A A + beta A + eye I
 };
@@ -59,13 +60,28 @@ __device__ __forceinline__ u32x2 pack4(const uint16_t (&h)[4]) {
   return u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
 }
 
-// Tile (tm, tn), tn <= tm, of entry t of the lower triangle taken row by row.
-__device__ __forceinline__ void tri_tile(int t, int& tm, int& tn) {
-  int r = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-  while (r * (r + 1) / 2 > t) --r;
-  while ((r + 1) * (r + 2) / 2 <= t) ++r;
-  tm = r;
-  tn = t - r * (r + 1) / 2;
+// Tile (tm, tn), tn <= tm < n, of entry t of the lower triangle, taken in strips of four
+// rows, column by column: neighbouring entries share row and column panels in L2 (a row
+// at a time, sixteen tiles in a row read sixteen column panels).
+__device__ __forceinline__ void tri_tile(int t, int n, int& tm, int& tn) {
+  for (int first = 0;; first += 4) {
+    const int h = min(4, n - first), square = first * h, count = square + h * (h + 1) / 2;
+    if (t >= count && first + 4 < n) {
+      t -= count;
+      continue;
+    }
+    if (t < square) {
+      tn = t / h;
+      tm = first + t % h;
+    } else {
+      t -= square;
+      int c = 0;
+      while (t >= h - c) t -= h - c++;
+      tn = first + c;
+      tm = first + c + t;
+    }
+    return;
+  }
 }
 
 template <int EDGE, bool BNC>
@@ -83,17 +99,46 @@ struct NsCore<128, BNC> {
   static constexpr int FM = G2SWave<BNC>::FM, FN = G2SWave<BNC>::FN, VEC = 1;
 };
 
-// V consecutive entries of row i.
-template <int V>
-__device__ __forceinline__ void load_f16(const uint16_t* p, float (&v)[V]) {
-  if constexpr (V == 4) {
-    const f16x4 h = *reinterpret_cast<const f16x4*>(p);
+__device__ __forceinline__ void unpack4(u32x2 w, float (&v)[4]) {
+  const f16x4 h = __builtin_bit_cast(f16x4, w);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (float)h[k];
-  } else {
-    v[0] = f16_to_f32(*p);
-  }
+  for (int k = 0; k < 4; ++k) v[k] = (float)h[k];
 }
+
+// What the epilogue adds at four rows (row .. row + 3) and VEC columns of an operand, as
+// loaded. Of a symmetric operand a lane with one column loads the four entries of row
+// `col` instead, which lie together.
+template <int VEC, bool SYM>
+struct NsBlock {
+  static constexpr int N = VEC == 4 ? 4 : SYM ? 1 : 2;
+  u32x2 w[N];
+  __device__ __forceinline__ void load(const uint16_t* p, int ld, int row, int col) {
+    if constexpr (VEC == 4) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w[r] = *reinterpret_cast<const u32x2*>(p + (int64_t)(row + r) * ld + col);
+    } else if constexpr (SYM) {
+      w[0] = *reinterpret_cast<const u32x2*>(p + (int64_t)col * ld + row);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) w[r >> 1][r & 1] = p[(int64_t)(row + r) * ld + col];
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[4][VEC]) const {
+    if constexpr (VEC == 4) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) unpack4(w[r], v[r]);
+    } else if constexpr (SYM) {
+      float t[4];
+      unpack4(w[0], t);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r][0] = t[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r][0] = f16_to_f32((uint16_t)w[r >> 1][r & 1]);
+    }
+  }
+};
+
 template <int V>
 __device__ __forceinline__ void store_f16(uint16_t* p, const uint16_t (&h)[V]) {
   if constexpr (V == 4) *reinterpret_cast<u32x2*>(p) = pack4(h);
@@ -103,111 +148,149 @@ __device__ __forceinline__ void store_f16(uint16_t* p, const uint16_t (&h)[V]) {
 // PAIR: operands and C are hi + lo, and a product is hi hi + hi lo + lo hi. Otherwise C =
 // (A + diag(a)) (B + diag(b)) = A B + (a_i B_ij + A_ij b_j) with the products of two
 // remainders left out, for square A (a) and B (b).
+//
+// Tiles of EDGE x EDGE, one a workgroup: those of the 256 grid from nbig on go as 128 x
+// 128 quarters, in a launch of their own (ns.hpp: ns_split).
+//
+// The 256 x 256 core leaves one workgroup a CU, so that whatever follows the K loop is
+// paid in full: the entries of A and B that the epilogue adds are loaded ahead, those of
+// the first rows before the K loop, the others while the rows before them are stored.
 template <int EDGE, bool FAST, int WHAT, bool PAIR>
 __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
   constexpr bool SYM = WHAT != kApplyX, BNC = WHAT != kGram;
   using Core = NsCore<EDGE, BNC>;
-  constexpr int VEC = Core::VEC;
+  constexpr int VEC = Core::VEC, FM = Core::FM, FN = Core::FN / VEC;
   __shared__ typename Core::Smem sm;
-  const int ntm = (g.M + EDGE - 1) / EDGE, ntn = (g.N + EDGE - 1) / EDGE;
-  int mat = blockIdx.x / g.tiles;
-  const int loc = xcd_remap((int)blockIdx.x - mat * g.tiles, g.tiles);
+  // ---- which tile
+  const int edge = g.nbig ? 256 : EDGE;  // of the grid that `tiles` counts
+  const int ntm = (g.M + edge - 1) / edge, ntn = (g.N + edge - 1) / edge;
+  const bool part = EDGE == 128 && g.nbig;
+  const int id = part ? g.nbig + (int)(blockIdx.x >> 2) : (int)blockIdx.x;
+  int mat = id / g.tiles;
+  const int loc = xcd_remap(id - mat * g.tiles, g.tiles);
   const int set = mat / g.count;
   mat -= set * g.count;
   int tm, tn;
   if constexpr (SYM)
-    tri_tile(loc, tm, tn);
+    tri_tile(loc, ntm, tm, tn);
   else
     grouped_tile(loc, ntm, ntn, 8, tm, tn);
   tm = to_scalar(tm);
   tn = to_scalar(tn);
   mat = to_scalar(mat);
-  const int m0 = tm * EDGE, n0 = tn * EDGE;
+  const int m0 = tm * edge + (part ? (blockIdx.x & 1) * 128 : 0), n0 = tn * edge + (part ? (blockIdx.x >> 1 & 1) * 128 : 0);
+  if (part && (m0 >= g.M || n0 >= g.N || (SYM && n0 > m0))) return;
   const NsMat a = set ? g.a[1] : g.a[0], b = set ? g.b[1] : g.b[0], c = set ? g.c[1] : g.c[0];
+  const uint16_t* ah = a.hi + mat * a.stride;
+  const uint16_t* bh = b.hi + mat * b.stride;
+  const typename Core::Map map;
+  // ---- what the epilogue adds: x of A (its low half xl for pairs), y of B
+  constexpr bool HAS_X = WHAT == kPoly || (WHAT == kMul && !PAIR), HAS_XL = WHAT == kPoly && PAIR;
+  constexpr bool HAS_Y = !PAIR && (WHAT == kMul || WHAT == kApplyX);
+  NsBlock<VEC, SYM> x[2][FN][4], xl[2][FN][4], y[2][FN][4];
+  NsBlock<VEC, SYM> xs[EDGE == 256 ? 1 : FM][FN][4], xls[EDGE == 256 ? 1 : FM][FN][4], ys[EDGE == 256 ? 1 : FM][FN][4];
+  auto inside = [&](int row, int col) { return FAST || (row < g.M && col < g.N); };  // (blocks are in or out)
+  // pairs leave the 256 x 256 core no registers to load ahead of the K loop, products of
+  // two operands' entries half of them
+  constexpr bool AHEAD_X = EDGE == 128 || !PAIR, AHEAD_Y = AHEAD_X && (EDGE == 128 || WHAT != kMul);
+  auto fetch = [&](int f, auto& bx, auto& bxl, auto& by, bool dox, bool doy) {
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = m0 + map.row(f, 4 * q), col = n0 + map.col(i * VEC);
+        if (!inside(row, col)) continue;
+        if constexpr (HAS_X) if (dox) bx[i][q].load(ah, g.ldc, row, col);
+        if constexpr (HAS_XL) if (dox) bxl[i][q].load(ah + a.lo_off, g.ldc, row, col);
+        if constexpr (HAS_Y) if (doy) by[i][q].load(bh, g.ldc, row, col);
+      }
+  };
+  if constexpr (EDGE == 256) {
+    fetch(0, x[0], xl[0], y[0], AHEAD_X, AHEAD_Y);
+  } else {
+#pragma unroll
+    for (int f = 0; f < FM; ++f) fetch(f, xs[f], xls[f], ys[f], true, true);
+  }
+  // ---- products
   f32x16 acc[Core::FM][Core::FN];
-  if constexpr (EDGE == 256)
+  const Operand A{ah + (int64_t)m0 * g.lda, g.lda, band_bytes(g.M - m0, g.lda) + (PAIR ? (uint32_t)(2 * a.lo_off) : 0u)};
+  const uint16_t* bp = bh + (BNC ? (int64_t)n0 : (int64_t)n0 * g.ldb);
+  const Operand B{bp, g.ldb,
+                  (BNC ? band_bytes(g.K, g.ldb, n0) : band_bytes(g.N - n0, g.ldb)) + (PAIR ? (uint32_t)(2 * b.lo_off) : 0u)};
+  if constexpr (EDGE == 256) {
     zero_acc2(acc);
-  else
-    zero_acc2s<BNC>(acc);
 #pragma unroll 1
-  for (int s = 0; s < (PAIR ? 3 : 1); ++s) {
-    const uint16_t* ap = (s == 2 ? a.lo : a.hi) + mat * a.stride + (int64_t)m0 * g.lda;
-    const uint16_t* bp = (s == 1 ? b.lo : b.hi) + mat * b.stride + (BNC ? (int64_t)n0 : (int64_t)n0 * g.ldb);
-    const Operand A{ap, g.lda, band_bytes(g.M - m0, g.lda)};
-    const Operand B{bp, g.ldb, BNC ? band_bytes(g.K, g.ldb, n0) : band_bytes(g.N - n0, g.ldb)};
-    if constexpr (EDGE == 256)
-      gemm2_mainloop<BNC, FAST, true>(sm, acc, A, B, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
-    else
+    for (int s = 0; s < (PAIR ? 3 : 1); ++s) {
+      const Operand As{A.base + (s == 2 ? a.lo_off : 0), A.ld, A.bytes - (s == 2 ? (uint32_t)(2 * a.lo_off) : 0u)};
+      const Operand Bs{B.base + (s == 1 ? b.lo_off : 0), B.ld, B.bytes - (s == 1 ? (uint32_t)(2 * b.lo_off) : 0u)};
+      gemm2_mainloop<BNC, FAST, true>(sm, acc, As, Bs, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
+    }
+  } else {
+    zero_acc2s<BNC>(acc);
+    if constexpr (PAIR) {
+      const K3 seg{g.K / 64, (uint32_t)(2 * a.lo_off), (uint32_t)(2 * b.lo_off)};
+      gemm2s_mainloop<BNC, true>(sm, acc, A, B, g.M - m0, g.N - n0, 3 * g.K, 0, 3 * (g.K / 64), seg);
+    } else {
       gemm2s_mainloop<BNC, true>(sm, acc, A, B, g.M - m0, g.N - n0, g.K, 0, g.K / 64);
+    }
   }
   // ---- epilogue (the mainloop ends with a barrier: LDS is free)
   const float alpha = set ? g.alpha[1] : g.alpha[0];
-  const typename Core::Map map;
   uint16_t* ch = c.hi + mat * c.stride;
-  uint16_t* cl = PAIR ? c.lo + mat * c.stride : nullptr;
-  const uint16_t* ah = a.hi + mat * a.stride;
-  const uint16_t* bh = b.hi + mat * b.stride;
-  const uint16_t* al = PAIR ? a.lo + mat * a.stride : nullptr;
   const float* ad = !PAIR && WHAT != kGram ? a.diag + mat * a.dstride : nullptr;
   const float* bd = !PAIR && (WHAT == kMul || WHAT == kPoly) ? b.diag + mat * b.dstride : nullptr;
   float* cd = !PAIR && SYM ? c.diag + mat * c.dstride : nullptr;
   // the tile is symmetric with tile (tn, tm): off the diagonal it is stored twice, the
   // second time transposed, by way of LDS so that whole lines are written
   constexpr bool STAGE = SYM && EDGE == 256 && !PAIR;
-  const bool mirror = SYM && tm != tn;
+  const bool mirror = SYM && m0 != n0;
   uint16_t* lds = reinterpret_cast<uint16_t*>(&sm);
+  auto finish = [&](int f, auto& bx, auto& bxl, auto& by) {
 #pragma unroll
-  for (int f = 0; f < Core::FM; ++f)
-#pragma unroll
-    for (int i = 0; i < Core::FN; i += VEC)
+    for (int i = 0; i < FN; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int lr = map.row(f, 4 * q), lc = map.col(i), row = m0 + lr, col = n0 + lc;
-        if (!FAST && (row >= g.M || col >= g.N)) continue;  // M and N are multiples of 64: blocks are in or out
-        uint16_t h[4][VEC], l[4][VEC];
-        float bdv[VEC];
+        const int lr = map.row(f, 4 * q), lc = map.col(i * VEC), row = m0 + lr, col = n0 + lc;
+        if (!inside(row, col)) continue;
+        float xv[4][VEC], yv[4][VEC], bdv[VEC];
+        f32x4 adv = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (HAS_X) bx[i][q].get(xv);
+        if constexpr (HAS_XL) {
+          bxl[i][q].get(yv);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) xv[r][k] += yv[r][k];
+        }
+        if constexpr (HAS_Y) by[i][q].get(yv);
+        if constexpr (!PAIR && WHAT != kGram) adv = *reinterpret_cast<const f32x4*>(ad + row);
         if constexpr (!PAIR && (WHAT == kMul || WHAT == kPoly)) {
 #pragma unroll
           for (int k = 0; k < VEC; ++k) bdv[k] = bd[col + k];
         }
+        uint16_t h[4][VEC], l[4][VEC];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int64_t at = (int64_t)(row + r) * g.ldc + col;
-          float v[VEC], x[VEC], y[VEC];
-          const float e = !PAIR && WHAT != kGram ? ad[row + r] : 0.f;
-          if constexpr (WHAT == kPoly) {
-            load_f16<VEC>(ah + at, x);
-            if constexpr (PAIR) {
-              load_f16<VEC>(al + at, y);
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) x[k] += y[k];
-            }
-          } else if constexpr (!PAIR && WHAT == kMul) {
-            load_f16<VEC>(ah + at, x);
-            load_f16<VEC>(bh + at, y);
-          } else if constexpr (!PAIR && WHAT == kApplyX) {
-            load_f16<VEC>(bh + at, y);
-          }
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            float t = acc[f][i + k][4 * q + r];
-            if constexpr (!PAIR && WHAT == kPoly) t = fmaf(e + bdv[k], x[k], t);
-            if constexpr (!PAIR && WHAT == kMul) t = fmaf(e, y[k], fmaf(bdv[k], x[k], t));
-            if constexpr (!PAIR && WHAT == kApplyX) t = fmaf(e, y[k], t);
+            float t = acc[f][i * VEC + k][4 * q + r];
+            if constexpr (!PAIR && WHAT == kPoly) t = fmaf(adv[r] + bdv[k], xv[r][k], t);
+            if constexpr (!PAIR && WHAT == kMul) t = fmaf(adv[r], yv[r][k], fmaf(bdv[k], xv[r][k], t));
+            if constexpr (!PAIR && WHAT == kApplyX) t = fmaf(adv[r], yv[r][k], t);
             t *= alpha;
             const bool on = SYM && row + r == col + k;
             if constexpr (WHAT == kPoly) {
-              t = fmaf(g.beta, x[k], t);
-              if (on) t += fmaf(g.beta, e, g.eye);
+              t = fmaf(g.beta, xv[r][k], t);
+              if (on) t += fmaf(g.beta, adv[r], g.eye);
             }
-            v[k] = t;
             h[r][k] = to_f16(t);
             const float rest = t - f16_to_f32(h[r][k]);
             if constexpr (PAIR) l[r][k] = to_f16(rest);
             if (!PAIR && on) cd[col + k] = rest;
           }
+          const int64_t at = (int64_t)(row + r) * g.ldc + col;
           store_f16<VEC>(ch + at, h[r]);
-          if constexpr (PAIR) store_f16<VEC>(cl + at, l[r]);
+          if constexpr (PAIR) store_f16<VEC>(ch + c.lo_off + at, l[r]);
         }
         if (SYM && mirror) {
 #pragma unroll
@@ -221,18 +304,30 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
               store_f16<4>(ch + at, ht);
               if constexpr (PAIR) {
                 const uint16_t lt[4] = {l[0][k], l[1][k], l[2][k], l[3][k]};
-                store_f16<4>(cl + at, lt);
+                store_f16<4>(ch + c.lo_off + at, lt);
               }
             }
           }
         }
       }
+  };
+  if constexpr (EDGE == 256) {
+    fetch(0, x[0], xl[0], y[0], !AHEAD_X, !AHEAD_Y);
+#pragma unroll
+    for (int f = 0; f < FM; ++f) {
+      if (f + 1 < FM) fetch(f + 1, x[(f + 1) & 1], xl[(f + 1) & 1], y[(f + 1) & 1], true, true);
+      finish(f, x[f & 1], xl[f & 1], y[f & 1]);
+    }
+  } else {
+#pragma unroll
+    for (int f = 0; f < FM; ++f) finish(f, xs[f], xls[f], ys[f]);
+  }
   if constexpr (STAGE) {
     if (!mirror) return;
     __syncthreads();
     const int p = threadIdx.x & 31;
     for (int cc = threadIdx.x >> 5; cc < 256; cc += 8)
-      if (FAST || (n0 + cc < g.N && m0 + 8 * p < g.M))
+      if (inside(m0 + 8 * p, n0 + cc))
         *reinterpret_cast<u32x4*>(ch + (int64_t)(n0 + cc) * g.ldc + m0 + 8 * p) =
             *reinterpret_cast<const u32x4*>(lds + cc * 256 + (p ^ (BNC ? (cc >> 2) & 31 : cc & 31)) * 8);
   }
@@ -337,7 +432,7 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   const int R = tall ? a.cols_m : a.rows_n, C = tall ? a.rows_n : a.cols_m;
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
   uint16_t* hi = X.hi + mat * X.stride;
-  uint16_t* lo = PAIR ? X.lo + mat * X.stride : nullptr;
+  uint16_t* lo = hi + X.lo_off;
   auto put = [&](int i, int j, f32x4 v) {
     u32x2 h, l;
 #pragma unroll
@@ -434,7 +529,7 @@ __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p,
   const int R = a.R[tall], C = a.C[tall];
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
   const uint16_t* hi = X.hi + mat * X.stride;
-  const uint16_t* lo = PAIR ? X.lo + mat * X.stride : nullptr;
+  const uint16_t* lo = hi + X.lo_off;
   const XTile<PAIR> xt{tile};
   if (tall) {
 #pragma unroll
@@ -531,11 +626,12 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
   const int64_t np = ns_pad(n), mp = ns_pad(m);
   auto mat = [&](int64_t rows, int64_t cols) {
     NsMat x{};
-    x.stride = rows * cols;
+    x.lo_off = rows * cols;
+    x.stride = rows * cols * (bf16 ? 1 : 2);
     x.dstride = rows;
     x.hi = (uint16_t*)take(2 * x.stride * count);
-    if (!bf16) x.lo = (uint16_t*)take(2 * x.stride * count);
-    else if (rows == np && cols == np) x.diag = (float*)take(4 * np * count);
+    if (!bf16) return x;
+    if (rows == np && cols == np) x.diag = (float*)take(4 * np * count);
     return x;
   };
   NsSpace s{};
@@ -558,23 +654,27 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
   } while (0)
 
 template <int EDGE, bool FAST, int WHAT, bool PAIR>
-void launch_gemm(const char* name, NsGemmArgs g, int sets, hipStream_t st) {
-  const int64_t ntm = ceil_div(g.M, EDGE), ntn = ceil_div(g.N, EDGE);
-  g.tiles = (int)(WHAT == kApplyX ? ntm * ntn : ntm * (ntm + 1) / 2);
-  FPO_LAUNCH(name, st,
-             (ns_gemm_kernel<EDGE, FAST, WHAT, PAIR><<<dim3((unsigned)(g.tiles * g.count * sets)), dim3(256), 0,
-                                                       st>>>(g)));
+void launch_gemm(const char* name, const NsGemmArgs& g, int64_t grid, hipStream_t st) {
+  FPO_LAUNCH(name, st, (ns_gemm_kernel<EDGE, FAST, WHAT, PAIR><<<dim3((unsigned)grid), dim3(256), 0, st>>>(g)));
 }
 
 template <int WHAT, bool PAIR>
-hipError_t launch_product(const char* name, const NsGemmArgs& g, int sets, hipStream_t st) {
+hipError_t launch_product(const char* name, NsGemmArgs g, int sets, hipStream_t st) {
   const int mats = g.count * sets;
-  if (!ns_big_tiles(g.M, g.N, (int64_t)g.K * (PAIR ? 3 : 1), mats, WHAT != kApplyX))
-    launch_gemm<128, false, WHAT, PAIR>(name, g, sets, st);
-  else if (g.M % 256 == 0 && g.N % 256 == 0)
-    launch_gemm<256, true, WHAT, PAIR>(name, g, sets, st);
-  else
-    launch_gemm<256, false, WHAT, PAIR>(name, g, sets, st);
+  const bool sym = WHAT != kApplyX;
+  const NsSplit sp = ns_split(g.M, g.N, (int64_t)g.K * (PAIR ? 3 : 1), mats, sym);
+  g.tiles = (int)ns_tiles(g.M, g.N, sp.nbig ? 256 : 128, sym);
+  const int64_t all = (int64_t)g.tiles * mats;
+  if (sp.nbig) {
+    if (g.M % 256 == 0 && g.N % 256 == 0)
+      launch_gemm<256, true, WHAT, PAIR>(name, g, sp.nbig, st);
+    else
+      launch_gemm<256, false, WHAT, PAIR>(name, g, sp.nbig, st);
+  }
+  if (sp.nbig < all) {
+    g.nbig = (int)sp.nbig;
+    launch_gemm<128, false, WHAT, PAIR>(name, g, sp.nbig ? 4 * (all - sp.nbig) : all, st);
+  }
   return hipGetLastError();
 }
 

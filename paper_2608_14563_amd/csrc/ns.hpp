@@ -141,17 +141,30 @@ inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
 }
 
 // ---------------------------------------------------------------- launch
-// Whether a launch of `mats` M x N products over K (symmetric: the tiles on and under the
-// diagonal) takes 256 x 256 tiles or 128 x 128 ones, by the estimates of big_tiles.
-inline bool ns_big_tiles(int64_t M, int64_t N, int64_t K, int64_t mats, bool symmetric) {
+// Tiles of one M x N product (symmetric: M == N, those on and under the diagonal).
+inline int64_t ns_tiles(int64_t M, int64_t N, int64_t edge, bool symmetric) {
+  const int64_t tm = ceil_div(M, edge), tn = ceil_div(N, edge);
+  return symmetric ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+// How a launch of `mats` M x N products over K is cut, as big_tiles does: the first nbig
+// 256 x 256 tiles as such, the others as 128 x 128 quarters; or (nbig 0) all as 128 x 128.
+struct NsSplit {
+  int64_t nbig;
+  double us;
+};
+inline NsSplit ns_split(int64_t M, int64_t N, int64_t K, int64_t mats, bool symmetric) {
   const double kt = (double)ceil_div(K, 64);
-  auto tiles = [&](int64_t edge) {
-    const int64_t tm = ceil_div(M, edge), tn = ceil_div(N, edge);
-    return mats * (symmetric ? tm * (tm + 1) / 2 : tm * tn);
-  };
-  const int64_t big = tiles(256), rem = big % kCus;
-  const double us = (double)(big / kCus) * (1.6 * kt + 14.0) + (rem ? (1.0 + 0.6 * (double)rem / kCus) * kt + 14.0 : 0.0);
-  return us <= (double)ceil_div(tiles(128), kCus) * (0.55 * kt + 7.5);
+  auto big = [&](int64_t n) { return n ? (1.0 + 0.6 * (double)n / kCus) * kt + 14.0 : 0.0; };
+  auto quarters = [&](int64_t n) { return (double)ceil_div(n, kCus) * (0.55 * kt + 7.5); };
+  const int64_t n = mats * ns_tiles(M, N, 256, symmetric), rem = n % kCus, whole = n - rem;
+  const double waves = (double)(n / kCus) * big(kCus);
+  NsSplit best{n, waves + big(rem)};
+  const double part = quarters(4 * rem) + 2.0;  // one more launch
+  if (whole && rem && part < 0.85 * big(rem)) best = NsSplit{whole, waves + part};
+  const double all = quarters(mats * ns_tiles(M, N, 128, symmetric));
+  if (all < 0.85 * best.us) best = NsSplit{0, all};
+  return best;
 }
 
 constexpr int kNsNormBlocks = 512;   // workgroups (and partials) a matrix of the norm pass
