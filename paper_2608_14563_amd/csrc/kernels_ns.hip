@@ -165,9 +165,13 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
   const int edge = g.nbig ? 256 : EDGE;  // of the grid that `tiles` counts
   const int ntm = (g.M + edge - 1) / edge, ntn = (g.N + edge - 1) / edge;
   const bool part = EDGE == 128 && g.nbig;
-  const int id = part ? g.nbig + (int)(blockIdx.x >> 2) : (int)blockIdx.x;
+  // a contiguous range of each 256 tiles to an XCD (which share its L2), all XCDs on the
+  // same matrices (which share the Infinity Cache)
+  const int win = (int)blockIdx.x & ~255;
+  const int slot = win + xcd_remap((int)blockIdx.x - win, min(256, (int)gridDim.x - win));
+  const int id = part ? g.nbig + (slot >> 2) : slot;
   int mat = id / g.tiles;
-  const int loc = xcd_remap(id - mat * g.tiles, g.tiles);
+  const int loc = id - mat * g.tiles;
   const int set = mat / g.count;
   mat -= set * g.count;
   int tm, tn;
@@ -178,7 +182,7 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
   tm = to_scalar(tm);
   tn = to_scalar(tn);
   mat = to_scalar(mat);
-  const int m0 = tm * edge + (part ? (blockIdx.x & 1) * 128 : 0), n0 = tn * edge + (part ? (blockIdx.x >> 1 & 1) * 128 : 0);
+  const int m0 = tm * edge + (part ? (slot & 1) * 128 : 0), n0 = tn * edge + (part ? (slot >> 1 & 1) * 128 : 0);
   if (part && (m0 >= g.M || n0 >= g.N || (SYM && n0 > m0))) return;
   const NsMat a = set ? g.a[1] : g.a[0], b = set ? g.b[1] : g.b[0], c = set ? g.c[1] : g.c[0];
   const uint16_t* ah = a.hi + mat * a.stride;
@@ -268,25 +272,35 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
 #pragma unroll
           for (int k = 0; k < VEC; ++k) bdv[k] = bd[col + k];
         }
+        float t[4][VEC];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {
+            t[r][k] = acc[f][i * VEC + k][4 * q + r];
+            if constexpr (!PAIR && WHAT == kPoly) t[r][k] = fmaf(adv[r] + bdv[k], xv[r][k], t[r][k]);
+            if constexpr (!PAIR && WHAT == kMul) t[r][k] = fmaf(adv[r], yv[r][k], fmaf(bdv[k], xv[r][k], t[r][k]));
+            if constexpr (!PAIR && WHAT == kApplyX) t[r][k] = fmaf(adv[r], yv[r][k], t[r][k]);
+            t[r][k] *= alpha;
+            if constexpr (WHAT == kPoly) t[r][k] = fmaf(g.beta, xv[r][k], t[r][k]);
+          }
+        if (SYM && !mirror) {  // (uniform) the diagonal's entries: the multiple of I, the remainders
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+              if (row + r == col + k) {
+                if constexpr (WHAT == kPoly) t[r][k] += fmaf(g.beta, adv[r], g.eye);
+                if constexpr (!PAIR) cd[col + k] = t[r][k] - f16_to_f32(to_f16(t[r][k]));
+              }
+        }
         uint16_t h[4][VEC], l[4][VEC];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            float t = acc[f][i * VEC + k][4 * q + r];
-            if constexpr (!PAIR && WHAT == kPoly) t = fmaf(adv[r] + bdv[k], xv[r][k], t);
-            if constexpr (!PAIR && WHAT == kMul) t = fmaf(adv[r], yv[r][k], fmaf(bdv[k], xv[r][k], t));
-            if constexpr (!PAIR && WHAT == kApplyX) t = fmaf(adv[r], yv[r][k], t);
-            t *= alpha;
-            const bool on = SYM && row + r == col + k;
-            if constexpr (WHAT == kPoly) {
-              t = fmaf(g.beta, xv[r][k], t);
-              if (on) t += fmaf(g.beta, adv[r], g.eye);
-            }
-            h[r][k] = to_f16(t);
-            const float rest = t - f16_to_f32(h[r][k]);
-            if constexpr (PAIR) l[r][k] = to_f16(rest);
-            if (!PAIR && on) cd[col + k] = rest;
+            h[r][k] = to_f16(t[r][k]);
+            if constexpr (PAIR) l[r][k] = to_f16(t[r][k] - f16_to_f32(h[r][k]));
           }
           const int64_t at = (int64_t)(row + r) * g.ldc + col;
           store_f16<VEC>(ch + at, h[r]);
