@@ -63,7 +63,13 @@ def _p(t: Optional[torch.Tensor], dtype: Optional[torch.dtype] = None, shape=Non
 F32, F64, I32 = torch.float32, torch.float64, torch.int32
 
 
+# the handle alone, without a stream object around it (0.06 us instead of 1.7)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(dev: torch.device) -> int:
+    if _raw_stream is not None and dev.index is not None:
+        return _raw_stream(dev.index)
     return torch.cuda.current_stream(dev).cuda_stream
 
 

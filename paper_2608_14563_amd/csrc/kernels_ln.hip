@@ -10,11 +10,14 @@
 //
 // A row is shared by 64 lanes (d up to 2048), 256 (up to 8192) or 1024 (up to 16384), each
 // holding up to four chunks of eight neighbouring elements; longer rows are read again for
-// every reduction. In the VJP a workgroup takes every grid-th row (group of four for 64 lanes)
-// and keeps its columns' sums of the two parameter gradients in registers; the workgroups'
-// sums go to the workspace and a second launch adds them in a fixed order (no atomics:
-// the same input gives the same bits). The next row is loaded before the current one's
-// reductions.
+// every reduction. In the VJP a workgroup takes every grid-th row (four at a time with 64
+// lanes) and keeps its columns' sums of the two parameter gradients in registers; the
+// workgroups' sums go to the workspace and a second launch adds them in a fixed order (no
+// atomics: the same input gives the same bits). The next row is loaded before the current
+// one's reductions. Next to HBM the vector instructions count too: some 14 an element in
+// the VJP, a third of the memory time if nothing waits, hence the products are shared
+// between the sums and gain is kept in registers. (64 lanes for d = 4096, 128 sums a lane
+// and one wave a SIMD, had nothing to hide a row's loads behind: 112 us against 90 for 256.)
 #include "common.hpp"
 #include "launch.hpp"
 #include "prof.hpp"
@@ -58,19 +61,33 @@ __device__ __forceinline__ float sum8(f32x8 v) {
 }
 
 // Sum over the LANES lanes of a row; 64 lanes: within the wave, else the workgroup is one
-// row's. `red` holds 2 floats a wave.
+// row's. `red` holds 3 x 16 floats.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* red) {
   if constexpr (LANES == 64) return wave_sum(v);
   else return block_sum(v, red);
 }
+// Three of them in one exchange.
 template <int LANES>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float* red) {
-  if constexpr (LANES == 64) {
-    a = wave_sum(a);
-    b = wave_sum(b);
-  } else {
-    block_sum2(a, b, red);
+__device__ __forceinline__ void row_sum3(float& a, float& b, float& c, float* red) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  c = wave_sum(c);
+  if constexpr (LANES > 64) {
+    const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+    __syncthreads();
+    if (l == 0) {
+      red[w] = a;
+      red[16 + w] = b;
+      red[32 + w] = c;
+    }
+    __syncthreads();
+    a = b = c = 0.f;
+    for (int i = 0; i < LANES / kWave; ++i) {  // fixed order
+      a += red[i];
+      b += red[16 + i];
+      c += red[32 + i];
+    }
   }
 }
 
@@ -164,7 +181,7 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
   constexpr int SLOTS = ln_threads(LANES) / LANES;
   constexpr int NR = NV ? NV : 1;
   constexpr bool AHEAD = NV > 0 && LANES < 1024;  // (1024 lanes have no registers left for it)
-  __shared__ float red[32];
+  __shared__ float red[48];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
   const T* x = (const T*)a.x;
   const TD* dy = (const TD*)a.dy;
@@ -197,6 +214,13 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
     }
     return g;
   };
+  constexpr bool KEEP_GAIN = (NV == 1 || NV == 2) && LANES < 1024;  // (else there are no registers left)
+  f32x8 gv[KEEP_GAIN ? NR : 1];
+  if constexpr (KEEP_GAIN) {
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+      if (lane + k * LANES < nc) gv[k] = gain8(lane + k * LANES);
+  }
   int64_t row = (int64_t)blockIdx.x * SLOTS + slot;
   if constexpr (AHEAD) {
     if (row < a.rows) fetch(row);
@@ -204,19 +228,21 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
   // with several slots a row's lanes are whole waves and nothing in the loop is a barrier
   for (; row < a.rows; row += step) {
     f32x8 vx[NR], vd[NR];
-    float s = 0.f;
-    auto each = [&](auto&& f) {  // f(chunk, k, x, dy)
+    auto each = [&](auto&& f) {  // f(chunk, k, x, dy, gain)
       if constexpr (NV > 0) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-          if (lane + k * LANES < nc) f(lane + k * LANES, k, vx[k], vd[k]);
+          if (lane + k * LANES < nc) {
+            if constexpr (KEEP_GAIN) f(lane + k * LANES, k, vx[k], vd[k], gv[k]);
+            else f(lane + k * LANES, k, vx[k], vd[k], gain8(lane + k * LANES));
+          }
       } else {
         for (int c = lane; c < nc; c += LANES) {
           Raw8<T> r;
           Raw8<TD> q;
           r.load(x + row * d + 8 * c);
           q.load(dy + row * d + 8 * c);
-          f(c, 0, r.get(), q.get());
+          f(c, 0, r.get(), q.get(), gain8(c));
         }
       }
     };
@@ -231,29 +257,39 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
     if constexpr (AHEAD) {
       if (row + step < a.rows) fetch(row + step);
     }
-    each([&](int, int, f32x8 t, f32x8) { s += sum8(t); });
+    float s = 0.f;
+    each([&](int, int, const f32x8& t, const f32x8&, const f32x8&) { s += sum8(t); });
     const float mean = row_sum<LANES>(s, red) * inv_d;
-    s = 0.f;
-    each([&](int, int, f32x8 t, f32x8) {
-      t -= mean;
-      s += sum8(t * t);
+    float ss[2] = {0.f, 0.f}, c1[2] = {0.f, 0.f}, c2[2] = {0.f, 0.f};  // of (x - mean)^2, v, v (x - mean)
+    each([&](int, int, const f32x8& t, const f32x8& g, const f32x8& gn) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xc = t[e] - mean;
+        ss[e & 1] = fmaf(xc, xc, ss[e & 1]);
+        c1[e & 1] = fmaf(g[e], gn[e], c1[e & 1]);
+        c2[e & 1] = fmaf(g[e] * xc, gn[e], c2[e & 1]);
+      }
     });
-    const float sigma = sqrtf(row_sum<LANES>(s, red) * inv_d + a.eps);
+    float sq = ss[0] + ss[1], m1 = c1[0] + c1[1], m2 = c2[0] + c2[1];
+    row_sum3<LANES>(sq, m1, m2, red);
+    const float sigma = sqrtf(sq * inv_d + a.eps);
     const float rstd = 1.f / sigma, inv = 1.f / fmaxf(sigma, a.min_std);
-    float c1 = 0.f, c2 = 0.f;
-    each([&](int c, int, f32x8 t, f32x8 g) {
-      const f32x8 v = g * gain8(c);
-      c1 += sum8(v);
-      c2 += sum8(v * ((t - mean) * inv));
-    });
-    row_sum2<LANES>(c1, c2, red);
-    c1 *= inv_d;
-    c2 *= inv_d;
-    each([&](int c, int k, f32x8 t, f32x8 g) {
-      const f32x8 xc = t - mean;
+    // dx = (v - mean v - x^ mean(v x^)) / sigma~ = inv v - o1 - o2 (x - mean)
+    const float o1 = m1 * inv_d * inv, o2 = m2 * inv_d * inv * inv * inv;
+    each([&](int c, int k, const f32x8& t, const f32x8& g, const f32x8& gn) {
+      f32x8 o, pr;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xc = t[e] - mean;
+        o[e] = fmaf(-o2, xc, fmaf(g[e], gn[e] * inv, -o1));
+        if constexpr (PARAM) pr[e] = g[e] * xc;
+      }
       if constexpr (PARAM && NV > 0) {
-        pg[k] += g * (xc * rstd);
-        pb[k] += g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          pg[k][e] = fmaf(pr[e], rstd, pg[k][e]);
+          pb[k][e] += g[e];
+        }
       } else if constexpr (PARAM) {
         const int64_t at = (int64_t)blockIdx.x * d + 8 * c;
         const bool add = row != (int64_t)blockIdx.x;  // not the workgroup's first row
@@ -266,10 +302,9 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
           }
           store8(p + at, w);
         };
-        keep(a.pgain, g * (xc * rstd));
+        keep(a.pgain, pr * rstd);
         keep(a.pbias, g);
       }
-      const f32x8 o = (g * gain8(c) - c1 - xc * inv * c2) * inv;
       if (a.dx) store8(a.dx + row * d + 8 * c, o);
       if (dx_lp) store8(dx_lp + row * d + 8 * c, o);
     });
@@ -305,35 +340,46 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
 }
 
 // Column sums of the workgroups' partials, dgain with blockIdx.y == 0, dbias with 1: 32
-// columns a workgroup, eight rows of partials at a time, added in double.
-__global__ __launch_bounds__(256) void ln_reduce_kernel(const float* __restrict__ pgain, const float* __restrict__ pbias,
+// columns (a line) a workgroup, 16 rows of partials at a time, added in double; eight
+// loads of a lane are in flight.
+__global__ __launch_bounds__(512) void ln_reduce_kernel(const float* __restrict__ pgain, const float* __restrict__ pbias,
                                                         int n, int d, float* dgain, float* dbias) {
-  __shared__ double part[8][32];
+  __shared__ double part[16][32];
   const float* p = blockIdx.y ? pbias : pgain;
   float* out = blockIdx.y ? dbias : dgain;
   if (!out) return;
   const int c = threadIdx.x % 32, r = threadIdx.x / 32, col = blockIdx.x * 32 + c;
   double s = 0.0;
-  if (col < d)
-    for (int i = r; i < n; i += 8) s += (double)p[(int64_t)i * d + col];
+  if (col < d) {
+    int i = r;
+    for (; i + 112 < n; i += 128) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p[(int64_t)(i + 16 * k) * d + col];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += (double)v[k];
+    }
+    for (; i < n; i += 16) s += (double)p[(int64_t)i * d + col];
+  }
   part[r][c] = s;
   __syncthreads();
   if (r == 0 && col < d) {
-    for (int i = 1; i < 8; ++i) s += part[i][c];
+    for (int i = 1; i < 16; ++i) s += part[i][c];
     out[col] = (float)s;
   }
 }
 
 constexpr int kLnForwardBlocks = 1 << 20;  // (a grid holds fewer than 2^32 lanes)
 constexpr int kLnBlocks = 2048;      // workgroups of the VJP without parameter gradients
-constexpr int kLnParamBlocks = 512;  // with them: each leaves a row of partials
 
 // How rows of d elements are held: lanes a row and chunks a lane (0: read again).
 struct LnShape {
   int lanes, nv;
 };
-LnShape ln_shape(int64_t d) {
+// Rows too few for four of them to a workgroup on every CU have a workgroup each.
+LnShape ln_shape(int64_t T, int64_t d) {
   const int64_t nc = d / 8;
+  if (nc > 64 && nc <= 256 && T < 4 * kCus) return {256, 1};
   if (nc <= 64) return {64, 1};
   if (nc <= 128) return {64, 2};
   if (nc <= 256) return {64, 4};
@@ -349,6 +395,7 @@ void with_shape(LnShape s, F&& f) {
   if (s.lanes == 64 && s.nv == 1) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
   else if (s.lanes == 64 && s.nv == 2) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
   else if (s.lanes == 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
+  else if (s.lanes == 256 && s.nv == 1) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
   else if (s.lanes == 256 && s.nv == 2) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
   else if (s.lanes == 256) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
   else if (s.nv == 2) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
@@ -364,7 +411,7 @@ void with_shape(LnShape s, F&& f) {
 template <typename T>
 hipError_t run_forward(const LnLaunch& a) {
   hipStream_t st = (hipStream_t)a.stream;
-  with_shape(ln_shape(a.d), [&](auto lanes, auto nv) {
+  with_shape(ln_shape(a.T, a.d), [&](auto lanes, auto nv) {
     constexpr int kThreads = ln_threads(lanes), kSlots = kThreads / lanes;
     FPO_LAUNCH("ln_forward", st,
                (ln_forward_kernel<T, lanes, nv><<<dim3((unsigned)std::min<int64_t>(ceil_div(a.T, kSlots), kLnForwardBlocks)), dim3(kThreads), 0, st>>>(
@@ -377,7 +424,7 @@ hipError_t run_forward(const LnLaunch& a) {
 template <typename T, typename TD>
 hipError_t run_vjp(const LnLaunch& a) {
   hipStream_t st = (hipStream_t)a.stream;
-  const LnShape sh = ln_shape(a.d);
+  const LnShape sh = ln_shape(a.T, a.d);
   const bool param = a.dgain || a.dbias;
   const int64_t groups = ceil_div(a.T, ln_threads(sh.lanes) / sh.lanes);
   const int n = param ? ln_vjp_blocks(a.T, a.d) : (int)std::min<int64_t>(groups, kLnBlocks);
@@ -396,7 +443,7 @@ hipError_t run_vjp(const LnLaunch& a) {
   FPO_CHECK_LAUNCH();
   if (param && !direct) {
     FPO_LAUNCH("ln_reduce", st,
-               ln_reduce_kernel<<<dim3((unsigned)ceil_div(a.d, 32), 2), dim3(256), 0, st>>>(v.pgain, v.pbias, n,
+               ln_reduce_kernel<<<dim3((unsigned)ceil_div(a.d, 32), 2), dim3(512), 0, st>>>(v.pgain, v.pbias, n,
                                                                                            (int)a.d, a.dgain, a.dbias));
     FPO_CHECK_LAUNCH();
   }
@@ -406,8 +453,10 @@ hipError_t run_vjp(const LnLaunch& a) {
 }  // namespace
 
 int ln_vjp_blocks(int64_t T, int64_t d) {
-  const LnShape s = ln_shape(d);
-  return (int)std::min<int64_t>(ceil_div(T, ln_threads(s.lanes) / s.lanes), kLnParamBlocks);
+  const LnShape s = ln_shape(T, d);
+  // as many workgroups a CU as their registers let run at once
+  const int per_cu = s.lanes == 256 && s.nv <= 2 ? 3 : 2;
+  return (int)std::min<int64_t>(ceil_div(T, ln_threads(s.lanes) / s.lanes), kCus * per_cu);
 }
 
 hipError_t launch_layernorm(const LnLaunch& a) {
