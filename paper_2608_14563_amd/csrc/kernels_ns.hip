@@ -18,71 +18,13 @@
 // 23 bits at three times the work, where fp32 matrix instructions take 16 times.
 #include "gemm2s.hpp"
 #include "gemm.hpp"
-#include "ns.hpp"
+#include "ns_dev.hpp"
 #include "prof.hpp"
 #include "upd.hpp"
 
 namespace fpo {
 
 namespace {
-
-// A stack of equal matrices in the workspace: fp16, or pairs of fp16. A square one of
-// single fp16 has `diag`: what its diagonal lost to rounding, in the same units.
-// These matrices are near multiples of I, their diagonals the largest entries, so half
-// of the rounding error of fp16 is there: 512 x 1382, five steps, 1.3e-3 against 64 bits
-// without it, 6.4e-4 with it.
-struct NsMat {
-  uint16_t* hi;
-  float* diag;
-  int64_t lo_off;   // elements from a hi to its lo (which follow each other)
-  int64_t stride;   // elements from one matrix to the next
-  int64_t dstride;  // of diag
-};
-
-// One launch of products C = alpha A B over `count` matrices, for one or two sets of operands.
-struct NsGemmArgs {
-  NsMat a[2], b[2], c[2];
-  int lda, ldb, ldc;
-  int M, N, K;         // padded sizes (multiples of 64)
-  int count, tiles;    // matrices; tiles a matrix
-  int nbig;            // 128 x 128 launch: the 256 x 256 tiles before it (0: all tiles are 128 x 128)
-  float alpha[2];      // by set
-  float beta, eye;     // kPoly: C = alpha A A + beta A + eye I
-};
-
-// What a launch computes. kGram: X X^T, B K-contiguous ([N][K] rows); the others have B
-// N-contiguous ([K][N]). kGram, kMul and kPoly: symmetric, tiles with tn <= tm. kApply: Q X.
-enum { kGram = 0, kMul = 1, kPoly = 2, kApplyX = 3 };
-
-__device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
-__device__ __forceinline__ float f16_to_f32(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
-__device__ __forceinline__ u32x2 pack4(const uint16_t (&h)[4]) {
-  return u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
-}
-
-// Tile (tm, tn), tn <= tm < n, of entry t of the lower triangle, taken in strips of four
-// rows, column by column: neighbouring entries share row and column panels in L2 (a row
-// at a time, sixteen tiles in a row read sixteen column panels).
-__device__ __forceinline__ void tri_tile(int t, int n, int& tm, int& tn) {
-  for (int first = 0;; first += 4) {
-    const int h = min(4, n - first), square = first * h, count = square + h * (h + 1) / 2;
-    if (t >= count && first + 4 < n) {
-      t -= count;
-      continue;
-    }
-    if (t < square) {
-      tn = t / h;
-      tm = first + t % h;
-    } else {
-      t -= square;
-      int c = 0;
-      while (t >= h - c) t -= h - c++;
-      tn = first + c;
-      tm = first + c + t;
-    }
-    return;
-  }
-}
 
 template <int EDGE, bool BNC>
 struct NsCore;
@@ -425,10 +367,12 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsEw a, NsPtrs p) {
   }
 }
 
-// X = 2^e u / (||u|| + eps) as fp16 (PAIR: hi + lo), n x m and padded with zeros; one 64 x 64
-// tile a workgroup. A tall matrix is transposed through LDS.
+// X = 2^e u / (||u|| + eps) as fp16 (PAIR: hi + lo), n x m and padded with zeros, and X^T
+// where it is wanted (XT.hi: small products, both then in their layout); one 64 x 64 tile
+// a workgroup. The matrix that is laid out
+// like the source (X, or X^T of a tall one) is stored as read, the other through LDS.
 template <typename T, bool MUON, bool PAIR>
-__global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat X, float pow2, int nblk) {
+__global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat X, NsMat XT, float pow2, int nblk) {
   __shared__ float tile[kNsEdge][kNsEdge + 1];
   __shared__ double red[4];
   const int mat = blockIdx.z, t = threadIdx.x;
@@ -445,9 +389,10 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   // source rows and columns of this tile
   const int R = tall ? a.cols_m : a.rows_n, C = tall ? a.rows_n : a.cols_m;
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
-  uint16_t* hi = X.hi + mat * X.stride;
-  uint16_t* lo = hi + X.lo_off;
-  auto put = [&](int i, int j, f32x4 v) {
+  const NsMat straight = tall ? XT : X, turned = tall ? X : XT;
+  const int ld_s = tall ? a.np : a.mp, ld_t = tall ? a.mp : a.np;
+  auto put = [&](const NsMat& to, int i, int j, int ld, f32x4 v) {
+    const int64_t at = XT.hi ? small_chunk(i, j & ~7, ld) + (j & 4) : (int64_t)i * ld + j;
     u32x2 h, l;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -455,9 +400,9 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
       h[k] = h0 | (uint32_t)h1 << 16;
       l[k] = to_f16(v[2 * k] - f16_to_f32(h0)) | (uint32_t)to_f16(v[2 * k + 1] - f16_to_f32(h1)) << 16;
     }
-    const int64_t at = (int64_t)i * a.mp + j;
-    *reinterpret_cast<u32x2*>(hi + at) = h;
-    if constexpr (PAIR) *reinterpret_cast<u32x2*>(lo + at) = l;
+    uint16_t* hi = to.hi + mat * to.stride + at;
+    *reinterpret_cast<u32x2*>(hi) = h;
+    if constexpr (PAIR) *reinterpret_cast<u32x2*>(hi + to.lo_off) = l;
   };
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -473,19 +418,18 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
       }
       v *= f;
     }
-    if (!tall) {
-      put(i0 + r, j0 + c, v);
-    } else {
+    if (straight.hi) put(straight, r0 + r, c0 + c, ld_s, v);
+    if (turned.hi) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) tile[r][c + q] = v[q];
     }
   }
-  if (!tall) return;
+  if (!turned.hi) return;
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int i = k * 16 + (t >> 4), j = 4 * (t & 15);
-    put(i0 + i, j0 + j, f32x4{tile[j][i], tile[j + 1][i], tile[j + 2][i], tile[j + 3][i]});
+    const int c = k * 16 + (t >> 4), r = 4 * (t & 15);
+    put(turned, c0 + c, r0 + r, ld_t, f32x4{tile[r][c], tile[r + 1][c], tile[r + 2][c], tile[r + 3][c]});
   }
 }
 
@@ -622,6 +566,7 @@ constexpr int64_t kNsAlign = 256;
 
 struct NsSpace {
   NsMat Xa, Xb;      // n x m: the iterates in turn
+  NsMat Xat, Xbt;    // m x n: their transposes, for small products only
   NsMat A, C, P[3];  // n x n: Gram matrix, B A, and three for B and the product of the B
   double* norm_part;
   double* part;
@@ -651,6 +596,10 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
   NsSpace s{};
   s.Xa = mat(np, mp);
   s.Xb = mat(np, mp);
+  if (ns_small(n, m, count, bf16)) {
+    s.Xat = mat(mp, np);
+    s.Xbt = mat(mp, np);
+  }
   s.A = mat(np, np);
   s.C = mat(np, np);
   for (auto& q : s.P) q = mat(np, np);
@@ -731,16 +680,17 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
                (ns_norm_kernel<float, true><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
     FPO_CHECK_LAUNCH();
     FPO_LAUNCH("ns_convert", st,
-               (ns_convert_kernel<float, true, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+               (ns_convert_kernel<float, true, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, s.Xat, pow_in, nblk)));
   } else {
     FPO_LAUNCH("ns_norm", st, (ns_norm_kernel<T, false><<<dim3(nblk, b.count), dim3(256), 0, st>>>(e, p)));
     FPO_CHECK_LAUNCH();
     FPO_LAUNCH("ns_convert", st,
-               (ns_convert_kernel<T, false, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, pow_in, nblk)));
+               (ns_convert_kernel<T, false, PAIR><<<tiles, dim3(256), 0, st>>>(e, p, s.Xa, s.Xat, pow_in, nblk)));
   }
   FPO_CHECK_LAUNCH();
 
-  NsMat X = s.Xa, Y = s.Xb;
+  NsMat X = s.Xa, Y = s.Xb, XT = s.Xat, YT = s.Xbt;
+  const bool small = XT.hi != nullptr;
   // C = 2^shift A B of square operands; more sets are added for the same launch
   const auto product = [&](const NsMat& l, const NsMat& r, const NsMat& out, double alpha) {
     NsGemmArgs g{};
@@ -753,6 +703,14 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     g.alpha[0] = (float)alpha;
     return g;
   };
+  const auto launch = [&](auto what, const char* name, const NsGemmArgs& g, int sets) {
+    constexpr int kWhat = decltype(what)::value;
+    return small ? launch_small_product(kWhat, name, g, sets, PAIR, NsMat{}, NsMat{}, 0, st)
+                 : launch_product<kWhat, PAIR>(name, g, sets, st);
+  };
+  constexpr std::integral_constant<int, kGram> gram;
+  constexpr std::integral_constant<int, kPoly> poly;
+  constexpr std::integral_constant<int, kMul> mul;
   hipError_t err;
   for (int gi = 0; gi < pl.ngroups; ++gi) {
     const NsGroup& gr = pl.groups[gi];
@@ -761,7 +719,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
       NsGemmArgs g = product(X, X, s.A, std::ldexp(1.0, sp[0].e_A - 2 * gr.e_X));
       g.lda = g.ldb = (int)mp;
       g.K = (int)mp;
-      if ((err = launch_product<kGram, PAIR>("ns_gram", g, 1, st)) != hipSuccess) return err;
+      if ((err = launch(gram, "ns_gram", g, 1)) != hipSuccess) return err;
     }
     int q = 0;  // P[q]: the product of the B so far; the other two are free
     for (int j = 0; j < gr.count; ++j) {
@@ -770,7 +728,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
         NsGemmArgs g = product(s.A, s.A, s.P[bj], sp[j].c * std::ldexp(1.0, sp[j].e_B - 2 * sp[j].e_A));
         g.beta = (float)(sp[j].b * std::ldexp(1.0, sp[j].e_B - sp[j].e_A));
         g.eye = (float)(sp[j].a * std::ldexp(1.0, sp[j].e_B));
-        if ((err = launch_product<kPoly, PAIR>("ns_poly", g, 1, st)) != hipSuccess) return err;
+        if ((err = launch(poly, "ns_poly", g, 1)) != hipSuccess) return err;
       }
       // the product of the B, and B A on the way to the next A = B A B, in one launch
       const bool more = j + 1 < gr.count;
@@ -783,10 +741,10 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
         g.c[sets] = s.P[qn];
         g.alpha[sets++] = (float)std::ldexp(1.0, sp[j].e_Q - sp[j].e_B - sp[j - 1].e_Q);
       }
-      if (sets && (err = launch_product<kMul, PAIR>("ns_mul", g, sets, st)) != hipSuccess) return err;
+      if (sets && (err = launch(mul, "ns_mul", g, sets)) != hipSuccess) return err;
       if (more) {
         g = product(s.C, s.P[bj], s.A, std::ldexp(1.0, sp[j + 1].e_A - sp[j].e_C - sp[j].e_B));
-        if ((err = launch_product<kMul, PAIR>("ns_mul", g, 1, st)) != hipSuccess) return err;
+        if ((err = launch(mul, "ns_mul", g, 1)) != hipSuccess) return err;
       }
       q = qn;
     }
@@ -795,8 +753,16 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     NsGemmArgs g = product(s.P[q], X, Y, std::ldexp(1.0, e_next - gr.e_X - sp[gr.count - 1].e_Q));
     g.ldb = g.ldc = (int)mp;
     g.N = (int)mp;
-    if ((err = launch_product<kApplyX, PAIR>("ns_apply", g, 1, st)) != hipSuccess) return err;
+    if (small) {
+      g.b[0] = XT;
+      const bool last = gi + 1 == pl.ngroups;
+      err = launch_small_product(kApplyX, "ns_apply", g, 1, PAIR, X, last ? NsMat{} : YT, last, st);
+    } else {
+      err = launch_product<kApplyX, PAIR>("ns_apply", g, 1, st);
+    }
+    if (err != hipSuccess) return err;
     std::swap(X, Y);
+    std::swap(XT, YT);
   }
 
   NsFinish f{};

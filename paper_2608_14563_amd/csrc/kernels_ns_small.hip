@@ -1,0 +1,218 @@
+// Newton-Schulz products of matrices too small to fill the chip with large tiles, where a
+// step is some twenty dependent launches and each launch's latency is what counts.
+//
+// A workgroup of 8 waves computes one 64 x 64 tile; the waves split K between them (every
+// eighth K step of 16 each), read their operands straight from memory and add their sums
+// in LDS. All of a wave's loads are in flight at once, two or four K steps ahead, so that
+// a launch takes little more than one memory latency, the sum and the store. Both operands
+// are read along K: a symmetric right operand is its own transpose, and X is kept both
+// ways. All matrices are stored in MFMA operands, blocks of 32 rows x 16 K entries, 1 KB
+// each in lane order (small_chunk): an operand is one contiguous load. (Row by row an
+// operand is 32 pieces of 32 bytes, and a launch took about twice as long.) All sides are
+// multiples of 64 here (padded with zeros), so nothing is checked.
+#include "gemm2.hpp"
+#include "ns_dev.hpp"
+#include "prof.hpp"
+
+namespace fpo {
+
+namespace {
+
+constexpr int kSmallWaves = 8, kSmallEdge = 64;
+constexpr int kRedLd = kSmallEdge + 4;  // row stride of the partial sums in LDS
+constexpr int kTrLd = kSmallEdge + 8;   // of the transposed tile
+
+// One K step's operands of a wave: 32 rows a fragment, 8 K entries a lane.
+template <bool PAIR>
+struct SmallFrag {
+  u32x4 a[2], b[2], al[PAIR ? 2 : 1], bl[PAIR ? 2 : 1];
+};
+
+__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+  const f16x8 h = __builtin_bit_cast(f16x8, w);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = (float)h[k];
+}
+__device__ __forceinline__ u32x4 pack8(const uint16_t (&h)[8]) {
+  return u32x4{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16,
+               h[6] | (uint32_t)h[7] << 16};
+}
+
+// rows: C is the caller's to read and stored row by row (kApplyX, the last one).
+template <int WHAT, bool PAIR>
+__global__ __launch_bounds__(64 * kSmallWaves) void ns_small_kernel(NsGemmArgs g, NsMat x_of_b, NsMat to_t, int rows) {
+  constexpr bool SYM = WHAT != kApplyX;
+  constexpr int U = PAIR ? 2 : 4;  // K steps loaded together
+  __shared__ float red[4][kSmallEdge][kRedLd];
+  const int ntm = g.M / kSmallEdge;
+  int mat = blockIdx.x / g.tiles;
+  const int loc = (int)blockIdx.x - mat * g.tiles;
+  const int set = mat / g.count;
+  mat -= set * g.count;
+  int tm, tn;
+  if constexpr (SYM) {
+    tri_tile(loc, ntm, tm, tn);
+  } else {
+    tn = loc / ntm;
+    tm = loc - tn * ntm;
+  }
+  const int m0 = tm * kSmallEdge, n0 = tn * kSmallEdge;
+  const NsMat a = set ? g.a[1] : g.a[0], b = set ? g.b[1] : g.b[0], c = set ? g.c[1] : g.c[0];
+  const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l = threadIdx.x & 63;
+  const uint16_t* ah = a.hi + mat * a.stride;
+  const uint16_t* bh = b.hi + mat * b.stride;
+  // ---- what the epilogue adds, eight entries of a row a thread, loaded ahead
+  const int er = threadIdx.x & 63, ec = 8 * (threadIdx.x >> 6);  // in the tile
+  const int row = m0 + er, col = n0 + ec;
+  const int64_t at = small_chunk(row, col, g.N);
+  u32x4 xw = {0u, 0u, 0u, 0u}, yw = xw;
+  float adv = 0.f, bdv[8];
+  if constexpr (WHAT == kPoly || (WHAT == kMul && !PAIR)) xw = *reinterpret_cast<const u32x4*>(ah + at);
+  if constexpr (WHAT == kPoly && PAIR) yw = *reinterpret_cast<const u32x4*>(ah + a.lo_off + at);
+  if constexpr (WHAT == kMul && !PAIR) yw = *reinterpret_cast<const u32x4*>(bh + at);
+  if constexpr (WHAT == kApplyX && !PAIR) yw = *reinterpret_cast<const u32x4*>(x_of_b.hi + mat * x_of_b.stride + at);
+  if constexpr (WHAT != kGram && !PAIR) adv = a.diag[mat * a.dstride + row];
+  if constexpr ((WHAT == kMul || WHAT == kPoly) && !PAIR) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) bdv[k] = b.diag[mat * b.dstride + col + k];
+  }
+  // ---- the wave's share of K
+  const int steps = g.K / 16;
+  const uint16_t* ap = ah + (int64_t)m0 * g.K + 8 * l;
+  const uint16_t* bp = bh + (int64_t)n0 * g.K + 8 * l;
+  const int64_t r32 = (int64_t)32 * g.K;  // the next 32 rows
+  f32x16 acc[2][2] = {{f32x16{}, f32x16{}}, {f32x16{}, f32x16{}}};
+  auto load = [&](SmallFrag<PAIR> (&f)[U], int s0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + kSmallWaves * u;
+      if (s >= steps) break;  // (uniform)
+      const uint16_t* pa = ap + 512 * (int64_t)s;
+      const uint16_t* pb = bp + 512 * (int64_t)s;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f[u].a[h] = *reinterpret_cast<const u32x4*>(pa + h * r32);
+        f[u].b[h] = *reinterpret_cast<const u32x4*>(pb + h * r32);
+        if constexpr (PAIR) {
+          f[u].al[h] = *reinterpret_cast<const u32x4*>(pa + h * r32 + a.lo_off);
+          f[u].bl[h] = *reinterpret_cast<const u32x4*>(pb + h * r32 + b.lo_off);
+        }
+      }
+    }
+  };
+  auto multiply = [&](const SmallFrag<PAIR> (&f)[U], int s0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + kSmallWaves * u >= steps) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          acc[h][i] = mfma_16bit<true>(f[u].a[h], f[u].b[i], acc[h][i]);
+          if constexpr (PAIR) {
+            acc[h][i] = mfma_16bit<true>(f[u].a[h], f[u].bl[i], acc[h][i]);
+            acc[h][i] = mfma_16bit<true>(f[u].al[h], f[u].b[i], acc[h][i]);
+          }
+        }
+    }
+  };
+  SmallFrag<PAIR> f0[U], f1[U];
+  constexpr int kAhead = kSmallWaves * U;
+  load(f0, w);
+  for (int s = w; s < steps; s += 2 * kAhead) {
+    load(f1, s + kAhead);
+    multiply(f0, s);
+    load(f0, s + 2 * kAhead);
+    multiply(f1, s + kAhead);
+  }
+  // ---- sums: waves 4..7 into LDS, added by waves 0..3, whose four are added below
+  const int lr = 4 * (l >> 5), lc = l & 31;
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) f(acc[h][i][r], red[w & 3][32 * h + 8 * (r >> 2) + lr + (r & 3)][32 * i + lc]);
+  };
+  if (w >= 4) each([](float v, float& m) { m = v; });
+  __syncthreads();
+  if (w < 4) each([](float v, float& m) { m += v; });
+  __syncthreads();
+  float t[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) t[k] = (red[0][er][ec + k] + red[1][er][ec + k]) + (red[2][er][ec + k] + red[3][er][ec + k]);
+  // ---- epilogue
+  const float alpha = set ? g.alpha[1] : g.alpha[0];
+  float xv[8], yv[8];
+  unpack8(xw, xv);
+  unpack8(yw, yv);
+  if constexpr (WHAT == kPoly && PAIR) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) xv[k] += yv[k];
+  }
+  uint16_t h[8], lo[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if constexpr (!PAIR && WHAT == kPoly) t[k] = fmaf(adv + bdv[k], xv[k], t[k]);
+    if constexpr (!PAIR && WHAT == kMul) t[k] = fmaf(adv, yv[k], fmaf(bdv[k], xv[k], t[k]));
+    if constexpr (!PAIR && WHAT == kApplyX) t[k] = fmaf(adv, yv[k], t[k]);
+    t[k] *= alpha;
+    if constexpr (WHAT == kPoly) {
+      t[k] = fmaf(g.beta, xv[k], t[k]);
+      if (row == col + k) t[k] += fmaf(g.beta, adv, g.eye);
+    }
+    h[k] = to_f16(t[k]);
+    const float rest = t[k] - f16_to_f32(h[k]);
+    if constexpr (PAIR) lo[k] = to_f16(rest);
+    if constexpr (!PAIR && SYM)
+      if (row == col + k) c.diag[mat * c.dstride + row] = rest;
+  }
+  uint16_t* ch = c.hi + mat * c.stride;
+  const int64_t out = rows ? (int64_t)row * g.N + col : at;
+  *reinterpret_cast<u32x4*>(ch + out) = pack8(h);
+  if constexpr (PAIR) *reinterpret_cast<u32x4*>(ch + c.lo_off + out) = pack8(lo);
+  // the transposed tile: C's other half, or C^T
+  const NsMat o = SYM ? c : to_t;
+  if (SYM ? m0 == n0 : o.hi == nullptr) return;
+  uint16_t* oh = o.hi + mat * o.stride;
+  uint16_t(*tr)[kSmallEdge][kTrLd] = reinterpret_cast<uint16_t(*)[kSmallEdge][kTrLd]>(&red[0][0][0]);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    tr[0][ec + k][er] = h[k];
+    if constexpr (PAIR) tr[1][ec + k][er] = lo[k];
+  }
+  __syncthreads();
+  const int64_t to = small_chunk(n0 + er, m0 + ec, g.M);
+  *reinterpret_cast<u32x4*>(oh + to) = *reinterpret_cast<const u32x4*>(&tr[0][er][ec]);
+  if constexpr (PAIR) *reinterpret_cast<u32x4*>(oh + o.lo_off + to) = *reinterpret_cast<const u32x4*>(&tr[1][er][ec]);
+}
+
+template <int WHAT>
+void launch_small(const char* name, const NsGemmArgs& g, int64_t grid, bool pair, const NsMat& x_of_b,
+                  const NsMat& to_t, int rows, hipStream_t st) {
+  if (pair)
+    FPO_LAUNCH(name, st,
+               (ns_small_kernel<WHAT, true><<<dim3((unsigned)grid), dim3(64 * kSmallWaves), 0, st>>>(g, x_of_b, to_t, rows)));
+  else
+    FPO_LAUNCH(name, st,
+               (ns_small_kernel<WHAT, false><<<dim3((unsigned)grid), dim3(64 * kSmallWaves), 0, st>>>(g, x_of_b, to_t, rows)));
+}
+
+}  // namespace
+
+hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
+                                const NsMat& to_t, int rows, hipStream_t st) {
+  g.tiles = (int)ns_tiles(g.M, g.N, kSmallEdge, what != kApplyX);
+  const int64_t grid = (int64_t)g.tiles * g.count * sets;
+  switch (what) {
+    case kGram: launch_small<kGram>(name, g, grid, pair, x_of_b, to_t, rows, st); break;
+    case kMul: launch_small<kMul>(name, g, grid, pair, x_of_b, to_t, rows, st); break;
+    case kPoly: launch_small<kPoly>(name, g, grid, pair, x_of_b, to_t, rows, st); break;
+    default: launch_small<kApplyX>(name, g, grid, pair, x_of_b, to_t, rows, st); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace fpo

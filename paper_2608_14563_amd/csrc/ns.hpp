@@ -167,6 +167,26 @@ inline NsSplit ns_split(int64_t M, int64_t N, int64_t K, int64_t mats, bool symm
   return best;
 }
 
+// Whether a batch of `count` matrices runs on 64 x 64 tiles (kernels_ns_small.hip): by the
+// least estimated time of the products of five steps in groups of 2, 1, 2. A round of 256
+// small tiles takes 3 us and 4.3 ns a K entry (pairs 3.4 and 9.5), a launch 1.2 us around it.
+// Measured, us small / large: fp16, 64 x 168 81 / 162, 512 x 1376 127 / 270, three of them
+// 157 / 283, eight 283 / 313; 1024 x 1024 158 / 310, three 311 / 327, eight 705 / 547;
+// 1536 x 4144 435 / 461. Pairs, 256 x 688 138 / 271, 512 x 1376 eight 474 / 474, 1280 x
+// 3456 487 / 839, three 1305 / 972.
+inline bool ns_small(int64_t n, int64_t m, int count, bool bf16) {
+  const int64_t np = ceil_div(n, 64) * 64, mp = ceil_div(m, 64) * 64;
+  const double round = bf16 ? 3.0 : 3.4, per_k = bf16 ? 0.0043 : 0.0095;
+  auto small = [&](int64_t N, int64_t K, bool sym) {
+    return (double)ceil_div(count * ns_tiles(np, N, 64, sym), kCus) * (round + per_k * (double)K) + 1.2;
+  };
+  auto large = [&](int64_t N, int64_t K, bool sym) {
+    return ns_split(np, N, K * (bf16 ? 1 : 3), count, sym).us + 1.5;
+  };
+  return 3 * small(np, mp, true) + 11 * small(np, np, true) + 3 * small(mp, np, false) <
+         3 * large(np, mp, true) + 11 * large(np, np, true) + 3 * large(mp, np, false);
+}
+
 constexpr int kNsNormBlocks = 512;   // workgroups (and partials) a matrix of the norm pass
 constexpr int kNsEdge = 64;          // edge of the tiles of the elementwise passes; n and m are padded to it
 

@@ -1,0 +1,80 @@
+// Device-side pieces that the kernels of the Newton-Schulz products share.
+#pragma once
+
+#include "common.hpp"
+#include "ns.hpp"
+
+namespace fpo {
+
+// A stack of equal matrices in the workspace: fp16, or pairs of fp16. A square one of
+// single fp16 has `diag`: what its diagonal lost to rounding, in the same units.
+// These matrices are near multiples of I, their diagonals the largest entries, so half
+// of the rounding error of fp16 is there: 512 x 1382, five steps, 1.3e-3 against 64 bits
+// without it, 6.4e-4 with it.
+struct NsMat {
+  uint16_t* hi;
+  float* diag;
+  int64_t lo_off;   // elements from a hi to its lo (which follow each other)
+  int64_t stride;   // elements from one matrix to the next
+  int64_t dstride;  // of diag
+};
+
+// One launch of products C = alpha A B over `count` matrices, for one or two sets of operands.
+struct NsGemmArgs {
+  NsMat a[2], b[2], c[2];
+  int lda, ldb, ldc;
+  int M, N, K;         // padded sizes (multiples of 64)
+  int count, tiles;    // matrices; tiles a matrix
+  int nbig;            // 128 x 128 launch: the 256 x 256 tiles before it (0: all tiles are 128 x 128)
+  float alpha[2];      // by set
+  float beta, eye;     // kPoly: C = alpha A A + beta A + eye I
+};
+
+// What a launch computes. kGram: X X^T, B K-contiguous ([N][K] rows); the others have B
+// N-contiguous ([K][N]). kGram, kMul and kPoly: symmetric, tiles with tn <= tm. kApply: Q X.
+enum { kGram = 0, kMul = 1, kPoly = 2, kApplyX = 3 };
+
+__device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+__device__ __forceinline__ float f16_to_f32(uint16_t h) { return (float)__builtin_bit_cast(_Float16, h); }
+__device__ __forceinline__ u32x2 pack4(const uint16_t (&h)[4]) {
+  return u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+}
+
+// Tile (tm, tn), tn <= tm < n, of entry t of the lower triangle, taken in strips of four
+// rows, column by column: neighbouring entries share row and column panels in L2 (a row
+// at a time, sixteen tiles in a row read sixteen column panels).
+__device__ __forceinline__ void tri_tile(int t, int n, int& tm, int& tn) {
+  for (int first = 0;; first += 4) {
+    const int h = min(4, n - first), square = first * h, count = square + h * (h + 1) / 2;
+    if (t >= count && first + 4 < n) {
+      t -= count;
+      continue;
+    }
+    if (t < square) {
+      tn = t / h;
+      tm = first + t % h;
+    } else {
+      t -= square;
+      int c = 0;
+      while (t >= h - c) t -= h - c++;
+      tn = first + c;
+      tm = first + c + t;
+    }
+    return;
+  }
+}
+
+// Where a small matrix (kernels_ns_small.hip) of `cols` columns has entries (row, col ..
+// col + 7), col a multiple of 8: blocks of 32 rows x 16 columns, in each the first eight
+// columns of the 32 rows, then the others.
+__device__ __forceinline__ int64_t small_chunk(int row, int col, int cols) {
+  return ((int64_t)(row >> 5) * (cols >> 4) + (col >> 4)) * 512 + ((col & 8) * 4 + (row & 31)) * 8;
+}
+
+// The products of small matrices: 64 x 64 tiles. B is given transposed: a symmetric one is
+// its own transpose, for kApplyX it is X^T, and x_of_b X itself. kApplyX stores C^T in to_t
+// if that has hi, and with `rows` C row by row.
+hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
+                                const NsMat& to_t, int rows, hipStream_t st);
+
+}  // namespace fpo

@@ -101,6 +101,46 @@ def test_orthogonalize_steps_and_coefficients(dev, steps, coefs, dtype):
     check(M, O, dtype, steps=steps, coefs=coefs)
 
 
+def newton_schulz_64(M, store=lambda x: x):
+    """The textbook iteration in float64 on the GPU (P.newton_schulz), `store` applied to
+    every matrix it keeps."""
+    X = M.double()
+    X = X if X.shape[0] <= X.shape[1] else X.t().contiguous()
+    X = X / (X.square().sum().sqrt() + 1e-7)
+    a, b, c = P.MUON_COEF
+    eye = torch.eye(X.shape[0], dtype=torch.float64, device=X.device)
+    for _ in range(5):
+        X = store(X)
+        A = store(X @ X.t())
+        X = store(a * eye + b * A + c * (A @ A)) @ X
+    return X if M.shape[0] <= M.shape[1] else X.t()
+
+
+# sizes and counts whose products run on each of the large tiles: 128 x 128; 256 x 256,
+# whole and at ragged edges; and those with the last ones as quarters
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,n", [(1032, 1096, 4), (1536, 1280, 8), (1288, 1544, 6), (2048, 2560, 8),
+                                         (2000, 1800, 8), (2048, 2048, 5)])
+def test_orthogonalize_large(dev, rows, cols, n, dtype):
+    """FPO_F32: a sum of K products rounds its accumulator 3 K times (three products), each
+    time by at most 2^-24 of it, at random sqrt(3 K) 2^-24 altogether; sixteen times that
+    for the five steps and what a group's B A B enlarges. FPO_BF16 as above."""
+    g = torch.Generator(device=dev)
+    g.manual_seed(rows + n)
+    M = [torch.randn(rows, cols, generator=g, device=dev).to(dtype) for _ in range(n)]
+    O = [torch.full_like(m, float("nan")) for m in M]
+    api.fpo_orthogonalize(M, O)
+    for i in (0, n // 2, n - 1):
+        E = newton_schulz_64(M[i])
+        if dtype == BF:
+            R = newton_schulz_64(M[i], lambda x: (x * 512).half().double() / 512)
+            tol = 2 * (R - E).norm() + 2 ** -8 * E.norm()
+        else:
+            tol = 16 * (3 * max(rows, cols)) ** 0.5 * 2 ** -24 * E.norm()
+        off = (O[i].double() - E).norm()
+        assert off <= tol, f"matrix {i}: off by {off:.3e}, allowed {tol:.3e}"
+
+
 def test_orthogonalize_mixed_batch(dev):
     """Matrices of several sizes and both orientations in one call, one of them zero:
     each as if alone, and a call with the workspace of the first one kept is the same bit for bit."""
