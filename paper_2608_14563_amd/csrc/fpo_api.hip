@@ -470,7 +470,7 @@ int check_ns(const fpo_ns_desc* d, int64_t n, const int64_t* rows, const int64_t
   if (n <= 0 || n > fpo::kMaxMats) return fail(FPO_ERR_SHAPE, "%s: n_mats must be in [1, %d]", who, fpo::kMaxMats);
   for (int64_t i = 0; d->coef && i < 3 * (int64_t)d->steps; ++i)
     if (!std::isfinite(d->coef[i])) return fail(FPO_ERR_ARG, "%s: coef must be finite", who);
-  if (!fpo::ns_plan(d->steps, d->coef, false).ok)
+  if (!fpo::ns_plan(d->steps, d->coef, 1).ok)
     return fail(FPO_ERR_ARG, "%s: these coefficients let a singular value grow past %g", who, fpo::kNsMaxSigma);
   for (int64_t m = 0; m < n; ++m) {
     if (rows[m] <= 0 || cols[m] <= 0 || rows[m] % 8 || cols[m] % 8 || rows[m] > kIntMax || cols[m] > kIntMax)

@@ -450,33 +450,7 @@ struct XTile {
   }
 };
 
-struct NsFinish {
-  int R[2], C[2];            // rows and columns of the caller's matrix: [0] wide, [1] tall
-  int mp;
-  uint64_t tall;
-  float pow2;                // 2^-e of X
-  int lp_bf16;
-  // muon
-  float decay, lr_wd;        // 1 - lr weight_decay, lr weight_decay
-  float step[2];             // lr times the scale of O, by orientation
-  int clip_update;
-  double clip_frac;
-  double* W_sumsq;
-  float* clip_scale;
-  double* part;              // [count][tiles]
-  double* dsq;               // [count] ||delta||^2
-};
-struct NsOutPtrs {
-  float* W[kMaxMats];
-  void* o[kMaxMats];         // O, or the low-precision copy of W
-  uint8_t id[kMaxMats];
-};
-
-enum { kWriteO = 0, kApply = 1, kDelta = 2 };
-
-// One 64 x 64 tile of the caller's matrix: O = X 2^-e written (kWriteO); the step on W,
-// W' = decay W - step O (kApply), or with the update clipped W' = W + k delta, delta =
-// -lr_wd W - step O; or the tile's share of ||delta||^2 (kDelta).
+// One 64 x 64 tile of the caller's matrix (finish4), and its share of a sum.
 template <typename T, int WHAT, bool PAIR>
 __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p, NsMat X) {
   __shared__ float tile[kNsEdge][kNsEdge + 1];
@@ -517,25 +491,7 @@ __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p,
       v = xt.load(hi, lo, (int64_t)(i0 + r) * a.mp + j0 + c);
     v *= a.pow2;
     const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
-    if constexpr (WHAT == kWriteO) {
-      st4<T>((T*)p.o[mat], at, v);
-    } else {
-      f32x4 w = ld4<float>(p.W[mat], at);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float delta = fmaf(-step, v[q], -a.lr_wd * w[q]);
-        if constexpr (WHAT == kDelta)
-          sum = fma((double)delta, (double)delta, sum);
-        else
-          w[q] = a.clip_update ? fmaf(k_clip, delta, w[q]) : fmaf(-step, v[q], a.decay * w[q]);
-      }
-      if constexpr (WHAT == kApply) {
-        st4<float>(p.W[mat], at, w);
-        if (p.o[mat]) st4<T>((T*)p.o[mat], at, w);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sum = fma((double)w[q], (double)w[q], sum);
-      }
-    }
+    finish4<T, WHAT>(a, p, mat, step, k_clip, at, v, sum);
   }
   if constexpr (WHAT != kWriteO) {
     sum = block_sum_d(sum, red);
@@ -596,7 +552,7 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
   NsSpace s{};
   s.Xa = mat(np, mp);
   s.Xb = mat(np, mp);
-  if (ns_small(n, m, count, bf16)) {
+  if (ns_choose(n, m, count, bf16).small) {
     s.Xat = mat(mp, np);
     s.Xbt = mat(mp, np);
   }
@@ -646,7 +602,8 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   hipStream_t st = (hipStream_t)a.stream;
   const int64_t n = b.n, m = b.m, np = ns_pad(n), mp = ns_pad(m);
   const NsSpace s = ns_carve(n, m, b.count, a.bf16, a.ws);
-  const NsPlan pl = ns_plan(a.steps, a.coef, ns_three_first(n, m, a.bf16));
+  const NsChoice choice = ns_choose(n, m, b.count, a.bf16);
+  const NsPlan pl = ns_plan(a.steps, a.coef, choice.first);
   NsPtrs p{};
   NsOutPtrs o{};
   for (int i = 0; i < b.count; ++i) {
@@ -689,6 +646,29 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   }
   FPO_CHECK_LAUNCH();
 
+  // what becomes of the last X
+  NsFinish f{};
+  f.R[0] = f.C[1] = (int)n;
+  f.C[0] = f.R[1] = (int)m;
+  f.mp = (int)mp;
+  f.tall = b.tall;
+  f.pow2 = (float)std::ldexp(1.0, -pl.e_out);
+  f.part = s.part;
+  f.dsq = s.dsq;
+  const auto scale = [&](double rows, double cols) {
+    return a.scale == kNsScaleRms        ? 0.2 * std::sqrt(std::max(rows, cols))
+           : a.scale == kNsScaleSpectral ? std::sqrt(std::max(1.0, rows / cols))
+                                         : 1.0;
+  };
+  f.step[0] = (float)(a.lr * scale((double)n, (double)m));
+  f.step[1] = (float)(a.lr * scale((double)m, (double)n));
+  f.decay = (float)(1.0 - a.lr * a.weight_decay);
+  f.lr_wd = (float)(a.lr * a.weight_decay);
+  f.clip_update = a.clip_update;
+  f.clip_frac = a.clip_frac;
+  f.W_sumsq = a.W_sumsq;
+  f.clip_scale = a.clip_scale;
+
   NsMat X = s.Xa, Y = s.Xb, XT = s.Xat, YT = s.Xbt;
   const bool small = XT.hi != nullptr;
   // C = 2^shift A B of square operands; more sets are added for the same launch
@@ -705,7 +685,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   };
   const auto launch = [&](auto what, const char* name, const NsGemmArgs& g, int sets) {
     constexpr int kWhat = decltype(what)::value;
-    return small ? launch_small_product(kWhat, name, g, sets, PAIR, NsMat{}, NsMat{}, 0, st)
+    return small ? launch_small_product(kWhat, name, g, sets, PAIR, NsMat{}, NsMat{}, false, nullptr, st)
                  : launch_product<kWhat, PAIR>(name, g, sets, st);
   };
   constexpr std::integral_constant<int, kGram> gram;
@@ -755,8 +735,11 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     g.N = (int)mp;
     if (small) {
       g.b[0] = XT;
-      const bool last = gi + 1 == pl.ngroups;
-      err = launch_small_product(kApplyX, "ns_apply", g, 1, PAIR, X, last ? NsMat{} : YT, last, st);
+      // the last one finishes the caller's matrices, unless the clip needs the whole step's norm first
+      const bool end = gi + 1 == pl.ngroups, fused = end && !a.clip_update;
+      const NsLast last{f, o, a.muon ? kApply : kWriteO};
+      err = launch_small_product(kApplyX, fused && a.muon ? "muon_apply" : "ns_apply", g, 1, PAIR, X, end ? NsMat{} : YT,
+                                 end, fused ? &last : nullptr, st);
     } else {
       err = launch_product<kApplyX, PAIR>("ns_apply", g, 1, st);
     }
@@ -765,32 +748,13 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     std::swap(XT, YT);
   }
 
-  NsFinish f{};
-  f.R[0] = f.C[1] = (int)n;
-  f.C[0] = f.R[1] = (int)m;
-  f.mp = (int)mp;
-  f.tall = b.tall;
-  f.pow2 = (float)std::ldexp(1.0, -pl.e_out);
-  f.part = s.part;
-  f.dsq = s.dsq;
   if (!a.muon) {
-    FPO_LAUNCH("ns_write", st, (ns_finish_kernel<T, kWriteO, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
-    FPO_CHECK_LAUNCH();
+    if (!small) {
+      FPO_LAUNCH("ns_write", st, (ns_finish_kernel<T, kWriteO, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
+      FPO_CHECK_LAUNCH();
+    }
     return hipSuccess;
   }
-  const auto scale = [&](double rows, double cols) {
-    return a.scale == kNsScaleRms        ? 0.2 * std::sqrt(std::max(rows, cols))
-           : a.scale == kNsScaleSpectral ? std::sqrt(std::max(1.0, rows / cols))
-                                         : 1.0;
-  };
-  f.step[0] = (float)(a.lr * scale((double)n, (double)m));
-  f.step[1] = (float)(a.lr * scale((double)m, (double)n));
-  f.decay = (float)(1.0 - a.lr * a.weight_decay);
-  f.lr_wd = (float)(a.lr * a.weight_decay);
-  f.clip_update = a.clip_update;
-  f.clip_frac = a.clip_frac;
-  f.W_sumsq = a.W_sumsq;
-  f.clip_scale = a.clip_scale;
   const int64_t ntiles = (np / kNsEdge) * (mp / kNsEdge);
   if (a.clip_update) {
     FPO_LAUNCH("muon_delta", st, (ns_finish_kernel<T, kDelta, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
@@ -799,8 +763,10 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
                ns_reduce_kernel<<<dim3(b.count), dim3(256), 0, st>>>(s.part, ntiles, s.dsq, nullptr, o));
     FPO_CHECK_LAUNCH();
   }
-  FPO_LAUNCH("muon_apply", st, (ns_finish_kernel<T, kApply, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
-  FPO_CHECK_LAUNCH();
+  if (!small || a.clip_update) {
+    FPO_LAUNCH("muon_apply", st, (ns_finish_kernel<T, kApply, PAIR><<<tiles, dim3(256), 0, st>>>(f, o, X)));
+    FPO_CHECK_LAUNCH();
+  }
   if (a.W_sumsq) {
     FPO_LAUNCH("muon_reduce", st,
                ns_reduce_kernel<<<dim3(b.count), dim3(256), 0, st>>>(s.part, ntiles, nullptr, a.W_sumsq, o));

@@ -91,14 +91,13 @@ inline double ns_value_max(double a, double b, double c, double top) {
 // where the singular values of a matrix of full rank also keep away from zero) and the
 // products' time is what counts (n >= 512: below, the launches' number, which is the
 // same); otherwise, and with pairs, whose point is accuracy, it takes two. After it
-// groups of one and two alternate. Coefficients that enlarge more close a group earlier
+// groups of one and two alternate, after one of three beginning with two. `first`: steps
+// in the first group, 1: one in each. Coefficients that enlarge more close a group earlier
 // (kNsGrowth is a little over 3.4445^4).
 constexpr double kNsGrowth = 150.0;
 constexpr double kNsMaxSigma = 1024.0;
 
-inline bool ns_three_first(int64_t n, int64_t m, bool bf16) { return bf16 && n >= 512 && 2 * m >= 3 * n; }
-
-inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
+inline NsPlan ns_plan(int steps, const double* coef, int first) {
   static const double kDefault[3] = {3.4445, -4.7750, 2.0315};
   NsPlan p;
   double r = 1.0;
@@ -116,7 +115,7 @@ inline NsPlan ns_plan(int steps, const double* coef, bool three_first) {
     p.steps[p.nsteps++] = s;
   }
   for (int i = 0; i < steps;) {
-    const int longest = i == 0 ? (three_first ? 3 : 2) : (p.ngroups % 2 == 1) != three_first ? 1 : 2;
+    const int longest = i == 0 || first == 1 ? first : p.ngroups % 2 == first % 2 ? 2 : 1;
     NsGroup g{i, 1, ns_exponent(p.steps[i].r_in)};
     double growth = p.steps[i].b_max * p.steps[i].b_max, q = p.steps[i].b_max;
     while (g.count < longest && i + g.count < steps && growth <= kNsGrowth) {
@@ -167,24 +166,36 @@ inline NsSplit ns_split(int64_t M, int64_t N, int64_t K, int64_t mats, bool symm
   return best;
 }
 
-// Whether a batch of `count` matrices runs on 64 x 64 tiles (kernels_ns_small.hip): by the
-// least estimated time of the products of five steps in groups of 2, 1, 2. A round of 256
-// small tiles takes 3 us and 4.3 ns a K entry (pairs 3.4 and 9.5), a launch 1.2 us around it.
-// Measured, us small / large: fp16, 64 x 168 81 / 162, 512 x 1376 127 / 270, three of them
-// 157 / 283, eight 283 / 313; 1024 x 1024 158 / 310, three 311 / 327, eight 705 / 547;
-// 1536 x 4144 435 / 461. Pairs, 256 x 688 138 / 271, 512 x 1376 eight 474 / 474, 1280 x
-// 3456 487 / 839, three 1305 / 972.
-inline bool ns_small(int64_t n, int64_t m, int count, bool bf16) {
+// How a batch of `count` matrices is computed: on 64 x 64 tiles (kernels_ns_small.hip) or
+// large ones, and the number of steps in the first group (ns_plan), by the least estimated
+// time of the products of five steps.
+//  * Up to 256 small tiles take 4.2 us and 4.3 ns a K entry (pairs 4.6 and 9.5), more of
+//    them 4.6 us and, per 256, 3.6 us and 2.1 ns a K entry (6 and 5.5). Measured, us small /
+//    large: fp16, 64 x 168 81 / 162, 512 x 1376 128 / 270, eight of them 242 / 313, 1024 x
+//    1024 158 / 310, eight 557 / 547, three 1280 x 3456 537 / 486. Pairs, 256 x 688 140 /
+//    271, eight 512 x 1376 402 / 474, three 1280 x 3456 1153 / 972.
+//  * One step a group takes three launches a step (15), groups of 2, 1, 2 take 17: fewer
+//    where a launch's latency is what counts.
+//  * Three steps in the first group of the large tiles: see ns_plan.
+struct NsChoice {
+  bool small;
+  int first;
+};
+inline double ns_small_us(int64_t tiles, int64_t K, bool bf16) {
+  if (tiles <= kCus) return bf16 ? 4.2 + 0.0043 * (double)K : 4.6 + 0.0095 * (double)K;
+  return 4.6 + (double)tiles / kCus * (bf16 ? 3.6 + 0.0021 * (double)K : 6.0 + 0.0055 * (double)K);
+}
+inline NsChoice ns_choose(int64_t n, int64_t m, int count, bool bf16) {
   const int64_t np = ceil_div(n, 64) * 64, mp = ceil_div(m, 64) * 64;
-  const double round = bf16 ? 3.0 : 3.4, per_k = bf16 ? 0.0043 : 0.0095;
-  auto small = [&](int64_t N, int64_t K, bool sym) {
-    return (double)ceil_div(count * ns_tiles(np, N, 64, sym), kCus) * (round + per_k * (double)K) + 1.2;
-  };
+  auto small = [&](int64_t N, int64_t K, bool sym) { return ns_small_us(count * ns_tiles(np, N, 64, sym), K, bf16); };
   auto large = [&](int64_t N, int64_t K, bool sym) {
     return ns_split(np, N, K * (bf16 ? 1 : 3), count, sym).us + 1.5;
   };
-  return 3 * small(np, mp, true) + 11 * small(np, np, true) + 3 * small(mp, np, false) <
-         3 * large(np, mp, true) + 11 * large(np, np, true) + 3 * large(mp, np, false);
+  const double g = small(np, mp, true), s = small(np, np, true), x = small(mp, np, false);
+  const double one = 5 * g + 5 * s + 5 * x, two = 3 * g + 11 * s + 3 * x;
+  const double big = 3 * large(np, mp, true) + 11 * large(np, np, true) + 3 * large(mp, np, false);
+  if (std::min(one, two) < big) return {true, one < two ? 1 : 2};
+  return {false, bf16 && n >= 512 && 2 * m >= 3 * n ? 3 : 2};
 }
 
 constexpr int kNsNormBlocks = 512;   // workgroups (and partials) a matrix of the norm pass

@@ -64,6 +64,58 @@ __device__ __forceinline__ void tri_tile(int t, int n, int& tm, int& tn) {
   }
 }
 
+// ---- what becomes of the orthogonal X
+struct NsFinish {
+  int R[2], C[2];            // rows and columns of the caller's matrix: [0] wide, [1] tall
+  int mp;
+  uint64_t tall;
+  float pow2;                // 2^-e of X
+  int lp_bf16;
+  // muon
+  float decay, lr_wd;        // 1 - lr weight_decay, lr weight_decay
+  float step[2];             // lr times the scale of O, by orientation
+  int clip_update;
+  double clip_frac;
+  double* W_sumsq;
+  float* clip_scale;
+  double* part;              // [count][tiles]
+  double* dsq;               // [count] ||delta||^2
+};
+struct NsOutPtrs {
+  float* W[kMaxMats];
+  void* o[kMaxMats];         // O, or the low-precision copy of W
+  uint8_t id[kMaxMats];
+};
+
+enum { kWriteO = 0, kApply = 1, kDelta = 2 };
+
+// Four entries v = O of the caller's matrix, from `at` on: written (kWriteO); the step on
+// W, W' = decay W - step O (kApply; sum: ||W'||^2), or with the update clipped W' = W + k
+// delta, delta = -lr_wd W - step O; or only ||delta||^2 (kDelta).
+template <typename T, int WHAT>
+__device__ __forceinline__ void finish4(const NsFinish& a, const NsOutPtrs& p, int mat, float step, float k, int64_t at,
+                                        f32x4 v, double& sum) {
+  if constexpr (WHAT == kWriteO) {
+    st4<T>((T*)p.o[mat], at, v);
+    return;
+  }
+  f32x4 w = ld4<float>(p.W[mat], at);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float delta = fmaf(-step, v[q], -a.lr_wd * w[q]);
+    if constexpr (WHAT == kDelta)
+      sum = fma((double)delta, (double)delta, sum);
+    else
+      w[q] = a.clip_update ? fmaf(k, delta, w[q]) : fmaf(-step, v[q], a.decay * w[q]);
+  }
+  if constexpr (WHAT == kApply) {
+    st4<float>(p.W[mat], at, w);
+    if (p.o[mat]) st4<T>((T*)p.o[mat], at, w);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum = fma((double)w[q], (double)w[q], sum);
+  }
+}
+
 // Where a small matrix (kernels_ns_small.hip) of `cols` columns has entries (row, col ..
 // col + 7), col a multiple of 8: blocks of 32 rows x 16 columns, in each the first eight
 // columns of the 32 rows, then the others.
@@ -73,8 +125,14 @@ __device__ __forceinline__ int64_t small_chunk(int row, int col, int cols) {
 
 // The products of small matrices: 64 x 64 tiles. B is given transposed: a symmetric one is
 // its own transpose, for kApplyX it is X^T, and x_of_b X itself. kApplyX stores C^T in to_t
-// if that has hi, and with `rows` C row by row.
+// if that has hi; with `rows` it stores C row by row, with `last` it does not store it but
+// finishes the caller's matrices (kWriteO or kApply).
+struct NsLast {
+  NsFinish f;
+  NsOutPtrs p;
+  int what;
+};
 hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
-                                const NsMat& to_t, int rows, hipStream_t st);
+                                const NsMat& to_t, bool rows, const NsLast* last, hipStream_t st);
 
 }  // namespace fpo

@@ -197,8 +197,8 @@ def test_binding_refusals():
 # --------------------------------------------------------------------- groups and exponents
 SRC = """
 #include "ns.hpp"
-extern "C" int plan(int steps, const double* coef, int three, int* out) {  // per group: count, e_X; per step: e_A, e_B, e_C, e_Q
-  const fpo::NsPlan p = fpo::ns_plan(steps, coef, three != 0);
+extern "C" int plan(int steps, const double* coef, int first, int* out) {  // per group: count, e_X; per step: e_A, e_B, e_C, e_Q
+  const fpo::NsPlan p = fpo::ns_plan(steps, coef, first);
   if (!p.ok) return -1;
   for (int i = 0; i < p.ngroups; ++i) { *out++ = p.groups[i].first; *out++ = p.groups[i].count; *out++ = p.groups[i].e_X; }
   for (int i = 0; i < p.nsteps; ++i) { const fpo::NsStep& s = p.steps[i]; *out++ = s.e_A; *out++ = s.e_B; *out++ = s.e_C; *out++ = s.e_Q; }
@@ -223,9 +223,9 @@ def host(tmp_path_factory):
     return lib
 
 
-def plan(host, steps, coef=None, three=False):
+def plan(host, steps, coef=None, first=2):
     out = (C.c_int * 512)()
-    n = host.plan(steps, (C.c_double * (3 * steps))(*coef) if coef else None, three, out)
+    n = host.plan(steps, (C.c_double * (3 * steps))(*coef) if coef else None, first, out)
     if n < 0:
         return None
     g = [tuple(out[3 * i:3 * i + 3]) for i in range(n)]
@@ -234,17 +234,18 @@ def plan(host, steps, coef=None, three=False):
 
 
 def test_groups(host):
-    counts = lambda k, three, c=None: [g[1] for g in plan(host, k, c, three)[0]]  # noqa: E731
-    for three in (False, True):
-        assert counts(1, three) == [1] and counts(2, three) == [2]
+    counts = lambda k, first, c=None: [g[1] for g in plan(host, k, c, first)[0]]  # noqa: E731
+    for first in (1, 2, 3):
+        assert counts(1, first) == [1] and counts(2, first) == [min(first, 2)] + [1] * (first == 1)
         # coefficients that enlarge more: groups close earlier
-        assert counts(3, three, (13.0, -40.0, 28.0) + (1.5, -0.5, 0.0) * 2)[0] == 1
+        assert counts(3, first, (13.0, -40.0, 28.0) + (1.5, -0.5, 0.0) * 2)[0] == 1
         for k in range(1, 33):
-            g = plan(host, k, None, three)[0]
+            g = plan(host, k, None, first)[0]
             assert sum(c for _, c, _ in g) == k
             assert [f for f, _, _ in g] == [sum(c for _, c, _ in g[:i]) for i in range(len(g))]
-    assert counts(3, False) == [2, 1] and counts(5, False) == [2, 1, 2] and counts(7, False) == [2, 1, 2, 1, 1]
-    assert counts(3, True) == [3] and counts(5, True) == [3, 2] and counts(7, True) == [3, 2, 1, 1]
+    assert counts(5, 1) == [1] * 5
+    assert counts(3, 2) == [2, 1] and counts(5, 2) == [2, 1, 2] and counts(7, 2) == [2, 1, 2, 1, 1]
+    assert counts(3, 3) == [3] and counts(5, 3) == [3, 2] and counts(7, 3) == [3, 2, 1, 1]
     assert plan(host, 2, (100.0, 0.0, 0.0) * 2) is None
 
 
@@ -261,7 +262,7 @@ def test_bounds_and_exponents(host):
             assert v <= host.value_max(a, b, c, top) * (1 + 1e-12) <= v * (1 + 1e-6) + 1e-12
             assert w <= host.poly_max(a, b, c, top * top) * (1 + 1e-12) <= w * (1 + 1e-6) + 1e-12
     for k, coef in ((5, None), (7, None), (3, (13.0, -40.0, 28.0) + (1.5, -0.5, 0.0) * 2), (12, (1.5, -0.5, 0.0) * 12)):
-        groups, steps, e_out = plan(host, k, coef, k % 2 == 1)
+        groups, steps, e_out = plan(host, k, coef, 3 if k % 2 else 2)
         lam = np.linspace(0, 1, 4001)  # eigenvalues of A
         for first, count, e_x in groups:
             assert np.sqrt(lam).max() * 2.0 ** e_x <= 2 ** 13
