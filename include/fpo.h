@@ -404,7 +404,8 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A,
  *
  *   n_mats      number of matrices (<= 64); any sizes together, those of equal
  *               (shorter, longer) side are computed in the same launches
- *   rows, cols  [host] int64 [n_mats], multiples of 8, rows * cols <= 2^29
+ *   rows, cols  [host] int64 [n_mats], multiples of 8; rows * cols, each
+ *               rounded up to 64, at most 2^29 (FPO_F32: 2^28)
  *   M           [host] n_mats pointers to [rows, cols] (dtype), read only
  *   O           [host] n_mats pointers to [rows, cols] (dtype), out; not aliasing M
  * dtype FPO_BF16: bf16 in and out; products of fp16 operands (scaled by powers of

@@ -458,7 +458,9 @@ hipError_t scratch_address(void** out) {
 }
 
 // ---------------------------------------------------------------- orthogonalisation
-constexpr int64_t kMaxMatNumel = (int64_t)1 << 29;  // operand bands stay below 2^31 bytes through 32-bit offsets
+// Entries of a matrix (sides rounded up to 64): operands, with row pitches and for float32
+// both halves, stay well below 2^31 bytes through 32-bit offsets.
+constexpr int64_t kMaxMatBytes = (int64_t)1 << 30;
 
 // The checks of desc and sizes that the workspace queries and the calls share.
 int check_ns(const fpo_ns_desc* d, int64_t n, const int64_t* rows, const int64_t* cols, const char* who) {
@@ -477,9 +479,9 @@ int check_ns(const fpo_ns_desc* d, int64_t n, const int64_t* rows, const int64_t
       return fail(FPO_ERR_SHAPE, "%s: sides of matrix %lld must be positive multiples of 8 (%lld x %lld)", who,
                   (long long)m, (long long)rows[m], (long long)cols[m]);
     // (padded sides: the elementwise passes' and products' tiles)
-    if (fpo::ns_pad(rows[m]) > kMaxMatNumel / fpo::ns_pad(cols[m]))
-      return fail(FPO_ERR_UNSUPPORTED, "%s: matrix %lld has more than 2^29 entries (sides rounded up to 64)", who,
-                  (long long)m);
+    if (fpo::ns_pad(rows[m]) > kMaxMatBytes / (d->dtype == FPO_BF16 ? 2 : 4) / fpo::ns_pad(cols[m]))
+      return fail(FPO_ERR_UNSUPPORTED, "%s: matrix %lld has more than 2^29 entries (float32: 2^28; sides rounded up to 64)",
+                  who, (long long)m);
   }
   return FPO_OK;
 }

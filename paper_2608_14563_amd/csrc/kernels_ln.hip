@@ -8,15 +8,16 @@
 // reductions over the lanes that share it (the squares are of differences from the
 // mean, so that a large mean costs no digits), and everything else is elementwise.
 //
-// A row is shared by 64 lanes (d up to 2048), 256 (up to 8192) or 1024 (up to 16384), each
-// holding up to four chunks of eight neighbouring elements; longer rows are read again for
-// every reduction. In the VJP a workgroup takes every grid-th row (four at a time with 64
-// lanes) and keeps its columns' sums of the two parameter gradients in registers; the
+// A row is shared by 64 lanes (d up to 1024 or 2048), 256 (up to 4096), 512 (8192) or 1024
+// (16384), each holding up to four chunks of eight neighbouring elements; longer rows are
+// read again for every reduction. A workgroup takes every grid-th row, loading the next
+// one before the current one's reductions, and keeps gain (and bias) in registers (8192 x
+// 4096 forward 32 -> 27 us: they were as many bytes from L2 as x and y). In the VJP
+// it also keeps its columns' sums of the two parameter gradients in registers; the
 // workgroups' sums go to the workspace and a second launch adds them in a fixed order (no
-// atomics: the same input gives the same bits). The next row is loaded before the current
-// one's reductions. Next to HBM the vector instructions count too: some 14 an element in
+// atomics: the same input gives the same bits). Next to HBM the vector instructions count too: some 14 an element in
 // the VJP, a third of the memory time if nothing waits, hence the products are shared
-// between the sums and gain is kept in registers. (64 lanes for d = 4096, 128 sums a lane
+// between the sums. (64 lanes for d = 4096, 128 sums a lane
 // and one wave a SIMD, had nothing to hide a row's loads behind: 112 us against 90 for 256.)
 #include "common.hpp"
 #include "launch.hpp"
@@ -91,7 +92,7 @@ __device__ __forceinline__ void row_sum3(float& a, float& b, float& c, float* re
   }
 }
 
-constexpr int ln_threads(int lanes) { return lanes == 1024 ? 1024 : 256; }
+constexpr int ln_threads(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // NV: chunks a lane (of 8 elements, LANES chunks apart); 0: any number, read again.
 template <typename T, int LANES, int NV>
@@ -105,53 +106,62 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_forward_kernel(const T* 
   constexpr int SLOTS = ln_threads(LANES) / LANES;
   const int nc = d / 8;
   const float inv_d = 1.f / (float)d;
+  constexpr int NR = NV ? NV : 1;
+  Raw8<T> rx[NR], rg[NR], rb[NR];  // the next row; gain and bias, kept for all of a workgroup's rows
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+      if (lane + k * LANES < nc) rx[k].load(x + row * d + 8 * (lane + k * LANES));
+  };
+  const int64_t step = (int64_t)gridDim.x * SLOTS;
+  int64_t row = (int64_t)blockIdx.x * SLOTS + slot;
+  if constexpr (NV > 0) {
+    if (row < rows) fetch(row);
+#pragma unroll
+    for (int k = 0; k < NR; ++k)
+      if (lane + k * LANES < nc) {
+        if (gain) rg[k].load(gain + 8 * (lane + k * LANES));
+        if (bias) rb[k].load(bias + 8 * (lane + k * LANES));
+      }
+  }
   // (with several slots a row's lanes are a whole wave, and nothing in the loop is a barrier)
-  for (int64_t row = (int64_t)blockIdx.x * SLOTS + slot; row < rows; row += (int64_t)gridDim.x * SLOTS) {
-    const T* xr = x + row * d;
-    f32x8 v[NV ? NV : 1];
+  for (; row < rows; row += step) {
+    f32x8 v[NR];
     float s = 0.f;
-    auto each = [&](auto&& f) {  // f(chunk, values): every chunk of the lane
+    auto each = [&](auto&& f) {  // f(chunk, k, values): every chunk of the lane
       if constexpr (NV > 0) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-          if (lane + k * LANES < nc) f(lane + k * LANES, v[k]);
+          if (lane + k * LANES < nc) f(lane + k * LANES, k, v[k]);
       } else {
         for (int c = lane; c < nc; c += LANES) {
           Raw8<T> r;
-          r.load(xr + 8 * c);
-          f(c, r.get());
+          r.load(x + row * d + 8 * c);
+          f(c, 0, r.get());
         }
       }
     };
     if constexpr (NV > 0) {
 #pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (lane + k * LANES < nc) {
-          Raw8<T> r;
-          r.load(xr + 8 * (lane + k * LANES));
-          v[k] = r.get();
-        }
+      for (int k = 0; k < NV; ++k) v[k] = rx[k].get();
+      if (row + step < rows) fetch(row + step);
     }
-    each([&](int, f32x8 t) { s += sum8(t); });
+    each([&](int, int, const f32x8& t) { s += sum8(t); });
     const float mean = row_sum<LANES>(s, red) * inv_d;
     s = 0.f;
-    each([&](int, f32x8 t) {
+    each([&](int, int, f32x8 t) {
       t -= mean;
       s += sum8(t * t);
     });
     const float rstd = 1.f / sqrtf(row_sum<LANES>(s, red) * inv_d + eps);
-    each([&](int c, f32x8 t) {
+    each([&](int c, int k, f32x8 t) {
       t = (t - mean) * rstd;
-      if (gain) {
-        Raw8<T> g;
-        g.load(gain + 8 * c);
-        t *= g.get();
+      if constexpr (NV == 0) {
+        if (gain) rg[0].load(gain + 8 * c);
+        if (bias) rb[0].load(bias + 8 * c);
       }
-      if (bias) {
-        Raw8<T> b;
-        b.load(bias + 8 * c);
-        t += b.get();
-      }
+      if (gain) t *= rg[k].get();
+      if (bias) t += rb[k].get();
       store8(y + row * d + 8 * c, t);
     });
     if (lane == 0) {
@@ -369,22 +379,25 @@ __global__ __launch_bounds__(512) void ln_reduce_kernel(const float* __restrict_
   }
 }
 
-constexpr int kLnForwardBlocks = 1 << 20;  // (a grid holds fewer than 2^32 lanes)
+constexpr int kLnForwardBlocks = 4 * kCus;  // workgroups of the forward pass
 constexpr int kLnBlocks = 2048;      // workgroups of the VJP without parameter gradients
 
 // How rows of d elements are held: lanes a row and chunks a lane (0: read again).
 struct LnShape {
   int lanes, nv;
 };
-// Rows too few for four of them to a workgroup on every CU have a workgroup each.
-LnShape ln_shape(int64_t T, int64_t d) {
+// Rows too few for four of them to a workgroup on every CU have a workgroup each. Between
+// 1032 and 2048 elements a wave a row is quicker in the forward pass (16384 x 2048: 26 us
+// against 33 with 256 lanes) and slower in the VJP, whose sums then leave one wave a SIMD
+// too few (84 against 72).
+LnShape ln_shape(int64_t T, int64_t d, bool vjp) {
   const int64_t nc = d / 8;
-  if (nc > 64 && nc <= 256 && T < 4 * kCus) return {256, 1};
+  const bool few = T < 4 * kCus;
   if (nc <= 64) return {64, 1};
-  if (nc <= 128) return {64, 2};
-  if (nc <= 256) return {64, 4};
+  if (nc <= 128) return few ? LnShape{256, 1} : LnShape{64, 2};
+  if (nc <= 256) return few || vjp ? LnShape{256, 1} : LnShape{64, 4};
   if (nc <= 512) return {256, 2};
-  if (nc <= 1024) return {256, 4};
+  if (nc <= 1024) return {512, 2};
   if (nc <= 2048) return {1024, 2};  // (1024 lanes leave 128 registers each)
   return {1024, 0};
 }
@@ -397,7 +410,7 @@ void with_shape(LnShape s, F&& f) {
   else if (s.lanes == 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   else if (s.lanes == 256 && s.nv == 1) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
   else if (s.lanes == 256 && s.nv == 2) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
-  else if (s.lanes == 256) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
+  else if (s.lanes == 512) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{});
   else if (s.nv == 2) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
   else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
@@ -411,7 +424,7 @@ void with_shape(LnShape s, F&& f) {
 template <typename T>
 hipError_t run_forward(const LnLaunch& a) {
   hipStream_t st = (hipStream_t)a.stream;
-  with_shape(ln_shape(a.T, a.d), [&](auto lanes, auto nv) {
+  with_shape(ln_shape(a.T, a.d, false), [&](auto lanes, auto nv) {
     constexpr int kThreads = ln_threads(lanes), kSlots = kThreads / lanes;
     FPO_LAUNCH("ln_forward", st,
                (ln_forward_kernel<T, lanes, nv><<<dim3((unsigned)std::min<int64_t>(ceil_div(a.T, kSlots), kLnForwardBlocks)), dim3(kThreads), 0, st>>>(
@@ -424,7 +437,7 @@ hipError_t run_forward(const LnLaunch& a) {
 template <typename T, typename TD>
 hipError_t run_vjp(const LnLaunch& a) {
   hipStream_t st = (hipStream_t)a.stream;
-  const LnShape sh = ln_shape(a.T, a.d);
+  const LnShape sh = ln_shape(a.T, a.d, true);
   const bool param = a.dgain || a.dbias;
   const int64_t groups = ceil_div(a.T, ln_threads(sh.lanes) / sh.lanes);
   const int n = param ? ln_vjp_blocks(a.T, a.d) : (int)std::min<int64_t>(groups, kLnBlocks);
@@ -453,9 +466,10 @@ hipError_t run_vjp(const LnLaunch& a) {
 }  // namespace
 
 int ln_vjp_blocks(int64_t T, int64_t d) {
-  const LnShape s = ln_shape(T, d);
-  // as many workgroups a CU as their registers let run at once
-  const int per_cu = s.lanes == 256 && s.nv <= 2 ? 3 : 2;
+  const LnShape s = ln_shape(T, d, true);
+  // about as many workgroups a CU as their registers let run at once; another one more has
+  // another row of partials to write and read
+  const int per_cu = s.lanes == 64 ? 2 : s.lanes == 256 ? (s.nv == 1 ? 3 : 2) : 1;
   return (int)std::min<int64_t>(ceil_div(T, ln_threads(s.lanes) / s.lanes), kCus * per_cu);
 }
 

@@ -309,7 +309,7 @@ struct NsPtrs {
 struct NsEw {
   int64_t numel;
   int rows_n, cols_m;        // n, m
-  int np, mp;                // padded
+  int np, mp;                // padded (mp on the large tiles: X's row pitch)
   uint64_t tall;
   double eps;
   float momentum;
@@ -539,20 +539,22 @@ NsSpace ns_carve(int64_t n, int64_t m, int count, bool bf16, void* ws) {
     return p;
   };
   const int64_t np = ns_pad(n), mp = ns_pad(m);
-  auto mat = [&](int64_t rows, int64_t cols) {
+  const bool small = ns_choose(n, m, count, bf16).small;
+  auto mat = [&](int64_t rows, int64_t width) {
+    const int64_t cols = small ? width : ns_pitch(width);
     NsMat x{};
     x.lo_off = rows * cols;
     x.stride = rows * cols * (bf16 ? 1 : 2);
     x.dstride = rows;
     x.hi = (uint16_t*)take(2 * x.stride * count);
     if (!bf16) return x;
-    if (rows == np && cols == np) x.diag = (float*)take(4 * np * count);
+    if (rows == np && width == np) x.diag = (float*)take(4 * np * count);
     return x;
   };
   NsSpace s{};
   s.Xa = mat(np, mp);
   s.Xb = mat(np, mp);
-  if (ns_choose(n, m, count, bf16).small) {
+  if (small) {
     s.Xat = mat(mp, np);
     s.Xbt = mat(mp, np);
   }
@@ -604,6 +606,8 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   const NsSpace s = ns_carve(n, m, b.count, a.bf16, a.ws);
   const NsChoice choice = ns_choose(n, m, b.count, a.bf16);
   const NsPlan pl = ns_plan(a.steps, a.coef, choice.first);
+  const bool small = choice.small;
+  const int64_t ldn = small ? np : ns_pitch(np), ldm = small ? mp : ns_pitch(mp);  // row pitches
   NsPtrs p{};
   NsOutPtrs o{};
   for (int i = 0; i < b.count; ++i) {
@@ -618,7 +622,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   e.rows_n = (int)n;
   e.cols_m = (int)m;
   e.np = (int)np;
-  e.mp = (int)mp;
+  e.mp = (int)ldm;
   e.tall = b.tall;
   e.eps = a.eps;
   e.momentum = a.momentum;
@@ -650,7 +654,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   NsFinish f{};
   f.R[0] = f.C[1] = (int)n;
   f.C[0] = f.R[1] = (int)m;
-  f.mp = (int)mp;
+  f.mp = (int)ldm;
   f.tall = b.tall;
   f.pow2 = (float)std::ldexp(1.0, -pl.e_out);
   f.part = s.part;
@@ -670,14 +674,13 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   f.clip_scale = a.clip_scale;
 
   NsMat X = s.Xa, Y = s.Xb, XT = s.Xat, YT = s.Xbt;
-  const bool small = XT.hi != nullptr;
   // C = 2^shift A B of square operands; more sets are added for the same launch
   const auto product = [&](const NsMat& l, const NsMat& r, const NsMat& out, double alpha) {
     NsGemmArgs g{};
     g.a[0] = l;
     g.b[0] = r;
     g.c[0] = out;
-    g.lda = g.ldb = g.ldc = (int)np;
+    g.lda = g.ldb = g.ldc = (int)ldn;
     g.M = g.N = g.K = (int)np;
     g.count = b.count;
     g.alpha[0] = (float)alpha;
@@ -697,7 +700,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     const NsStep* sp = &pl.steps[gr.first];
     {  // A = X X^T
       NsGemmArgs g = product(X, X, s.A, std::ldexp(1.0, sp[0].e_A - 2 * gr.e_X));
-      g.lda = g.ldb = (int)mp;
+      g.lda = g.ldb = (int)ldm;
       g.K = (int)mp;
       if ((err = launch(gram, "ns_gram", g, 1)) != hipSuccess) return err;
     }
@@ -731,7 +734,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
     // X <- Q X
     const int e_next = gi + 1 < pl.ngroups ? pl.groups[gi + 1].e_X : pl.e_out;
     NsGemmArgs g = product(s.P[q], X, Y, std::ldexp(1.0, e_next - gr.e_X - sp[gr.count - 1].e_Q));
-    g.ldb = g.ldc = (int)mp;
+    g.ldb = g.ldc = (int)ldm;
     g.N = (int)mp;
     if (small) {
       g.b[0] = XT;

@@ -67,7 +67,7 @@ __device__ __forceinline__ void tri_tile(int t, int n, int& tm, int& tn) {
 // ---- what becomes of the orthogonal X
 struct NsFinish {
   int R[2], C[2];            // rows and columns of the caller's matrix: [0] wide, [1] tall
-  int mp;
+  int mp;                    // X's row pitch
   uint64_t tall;
   float pow2;                // 2^-e of X
   int lp_bf16;

@@ -52,6 +52,8 @@ def test_orthogonalize_refusals(lib):
         assert orth(lib, ns(), rows=(r,), cols=(c,)) == L.FPO_ERR_SHAPE
     assert orth(lib, ns(), rows=(1 << 15,), cols=((1 << 14) + 8,)) == L.FPO_ERR_UNSUPPORTED
     assert orth(lib, ns(), rows=(8,), cols=((1 << 23) + 8,)) == L.FPO_ERR_UNSUPPORTED  # 8 rows take 64
+    assert orth(lib, ns(L.FPO_F32), rows=(1 << 14,), cols=((1 << 14) + 8,)) == L.FPO_ERR_UNSUPPORTED
+    assert orth(lib, ns(L.FPO_F32), rows=(1 << 14,), cols=(1 << 14,), ws=None) == L.FPO_ERR_WORKSPACE
     for s in (0, -1, 33):
         assert orth(lib, ns(steps=s)) == L.FPO_ERR_ARG
     for e in (-1e-9, math.nan, math.inf):
