@@ -407,7 +407,8 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A,
  *   rows, cols  [host] int64 [n_mats], multiples of 8; rows * cols, each
  *               rounded up to 64, at most 2^29 (FPO_F32: 2^28)
  *   M           [host] n_mats pointers to [rows, cols] (dtype), read only
- *   O           [host] n_mats pointers to [rows, cols] (dtype), out; not aliasing M
+ *   O           [host] n_mats pointers to [rows, cols] (dtype), out; no buffer twice,
+ *               and none that overlaps a matrix of M
  * dtype FPO_BF16: bf16 in and out; products of fp16 operands (scaled by powers of
  * two, more digits than bf16), fp32 accumulation. FPO_F32: float32 in and out,
  * products to about fp32 precision (pairs of fp16, three products).
@@ -451,7 +452,8 @@ int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* ro
  *   upd         W_master, state1 (momentum; may be NULL, the array or an entry, if
  *               momentum is 0), W_lp (dtype desc->ns.dtype), clip_scale as in
  *               fpo_update_bufs; W_sumsq may be NULL if clip_frac <= 0, else (and
- *               whenever given) in ||W||_F^2, out ||W'||_F^2; state2 is ignored
+ *               whenever given) in ||W||_F^2, out ||W'||_F^2; state2 is ignored. No
+ *               buffer may be given for two matrices
  * ns.dtype sets the precision of the products and the type of W_lp; everything else
  * is float32.
  * Returns FPO_OK or an fpo_status. */
@@ -478,7 +480,8 @@ int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, co
  *   x, y        [T, d] (dtype); y must not alias x
  *   gain, bias  [d] (dtype), each nullable: ones, zeros
  *   mean, rstd  float [T] out, nullable: mu and 1 / sigma
- * T <= 2^23, d a multiple of 8, d <= 2^22.
+ * T <= 2^23, d a multiple of 8, d <= 2^22. The statistics are float32: entries up to
+ * about 1e18 / sqrt(d) from the mean, whose squares can still be added.
  * Returns FPO_OK or an fpo_status. */
 typedef struct {
   int64_t T, d;

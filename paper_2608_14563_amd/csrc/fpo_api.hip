@@ -528,6 +528,16 @@ size_t ns_ws(bool bf16, int64_t n, const int64_t* rows, const int64_t* cols) {
   return need;
 }
 
+// Buffers that a call writes: the matrices are computed together, so none may be given twice.
+int check_distinct(const void* const* p, int64_t n, const char* who, const char* name) {
+  for (int64_t i = 0; i < n; ++i)
+    for (int64_t j = 0; j < i; ++j)
+      if (p[i] && p[i] == p[j])
+        return fail(FPO_ERR_ARG, "%s: %s of matrices %lld and %lld are the same buffer", who, name, (long long)j,
+                    (long long)i);
+  return FPO_OK;
+}
+
 int check_muon(const fpo_muon* o) {
   if (!o) return fail(FPO_ERR_NULL, "fpo_muon_update: opt is NULL");
   if (!(o->lr >= 0.0) || !std::isfinite(o->lr)) return fail(FPO_ERR_ARG, "fpo_muon_update: lr must be finite and >= 0");
@@ -918,6 +928,11 @@ int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* ro
     if (!aligned(M[m], 16) || !aligned(O[m], 16))
       return fail(FPO_ERR_ARG, "fpo_orthogonalize: buffers of matrix %lld must be 16-byte aligned", (long long)m);
   }
+  if (int e = check_distinct(O, n_mats, "fpo_orthogonalize", "O")) return e;
+  for (int64_t i = 0; i < n_mats; ++i)
+    for (int64_t j = 0; j < n_mats; ++j)  // (one batch's O is written before the next one's M is read)
+      if (O[i] == M[j])
+        return fail(FPO_ERR_ARG, "fpo_orthogonalize: O of matrix %lld is M of matrix %lld", (long long)i, (long long)j);
   const bool bf16 = desc->dtype == FPO_BF16;
   if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_orthogonalize")) return e;
   fpo::NsLaunch L{};
@@ -961,6 +976,11 @@ int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, co
       return fail(FPO_ERR_ARG, "fpo_muon_update: buffers of matrix %lld must be 16-byte aligned (bf16 W_lp: 8)",
                   (long long)m);
   }
+  if (int e = check_distinct((const void* const*)upd->W_master, n_mats, "fpo_muon_update", "W_master")) return e;
+  if (upd->W_lp)
+    if (int e = check_distinct(upd->W_lp, n_mats, "fpo_muon_update", "W_lp")) return e;
+  if (upd->state1)
+    if (int e = check_distinct((const void* const*)upd->state1, n_mats, "fpo_muon_update", "state1")) return e;
   if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_muon_update")) return e;
   fpo::NsLaunch L{};
   L.steps = opt->ns.steps;

@@ -12,13 +12,14 @@
 // (16384), each holding up to four chunks of eight neighbouring elements; longer rows are
 // read again for every reduction. A workgroup takes every grid-th row, loading the next
 // one before the current one's reductions, and keeps gain (and bias) in registers (8192 x
-// 4096 forward 32 -> 27 us: they were as many bytes from L2 as x and y). In the VJP
-// it also keeps its columns' sums of the two parameter gradients in registers; the
+// 4096 bf16 forward 32 -> 27 us, 5.0 TB/s: they were as many bytes from L2 as x and y). In
+// the VJP it also keeps its columns' sums of the two parameter gradients in registers; the
 // workgroups' sums go to the workspace and a second launch adds them in a fixed order (no
-// atomics: the same input gives the same bits). Next to HBM the vector instructions count too: some 14 an element in
-// the VJP, a third of the memory time if nothing waits, hence the products are shared
-// between the sums. (64 lanes for d = 4096, 128 sums a lane
-// and one wave a SIMD, had nothing to hide a row's loads behind: 112 us against 90 for 256.)
+// atomics: the same input gives the same bits). Next to HBM the vector instructions count
+// too, some 14 an element in the VJP, a third of the memory time if nothing waits; hence
+// the products are shared between the sums (8192 x 4096, bf16 x and dx_lp, float32 dy and
+// dx: 87 us, 4.6 TB/s; a wave a row, 128 sums a lane and one wave a SIMD, had nothing to
+// hide a row's loads behind, 112 us).
 #include "common.hpp"
 #include "launch.hpp"
 #include "prof.hpp"
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(512) void ln_reduce_kernel(const float* __restrict_
 }
 
 constexpr int kLnForwardBlocks = 4 * kCus;  // workgroups of the forward pass
-constexpr int kLnBlocks = 2048;      // workgroups of the VJP without parameter gradients
+constexpr int kLnBlocks = 2048;              // workgroups of the VJP without parameter gradients
 
 // How rows of d elements are held: lanes a row and chunks a lane (0: read again).
 struct LnShape {
@@ -426,8 +427,9 @@ hipError_t run_forward(const LnLaunch& a) {
   hipStream_t st = (hipStream_t)a.stream;
   with_shape(ln_shape(a.T, a.d, false), [&](auto lanes, auto nv) {
     constexpr int kThreads = ln_threads(lanes), kSlots = kThreads / lanes;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.T, kSlots), kLnForwardBlocks));
     FPO_LAUNCH("ln_forward", st,
-               (ln_forward_kernel<T, lanes, nv><<<dim3((unsigned)std::min<int64_t>(ceil_div(a.T, kSlots), kLnForwardBlocks)), dim3(kThreads), 0, st>>>(
+               (ln_forward_kernel<T, lanes, nv><<<grid, dim3(kThreads), 0, st>>>(
                    (const T*)a.x, (const T*)a.gain, (const T*)a.bias, a.T, (int)a.d, a.eps, (T*)a.y, a.mean, a.rstd)));
   });
   FPO_CHECK_LAUNCH();

@@ -34,7 +34,7 @@ def ns(dtype=L.FPO_BF16, steps=5, eps=1e-7, coef=None):
     return L.NsDesc(dtype, steps, eps, (C.c_double * len(coef))(*coef) if coef else None)
 
 
-def orth(lib, desc, n=1, rows=(64,), cols=(128,), M=(FAKE,), O=(FAKE,), ws=FAKE, ws_bytes=1 << 40):
+def orth(lib, desc, n=1, rows=(64,), cols=(128,), M=(FAKE,), O=(FAKE + 4096,), ws=FAKE, ws_bytes=1 << 40):
     return lib.fpo_orthogonalize(C.byref(desc) if desc else None, n, i64(*rows) if rows else None,
                                  i64(*cols) if cols else None, ptrs(*M) if M else None, ptrs(*O) if O else None, ws,
                                  ws_bytes, None)
@@ -68,6 +68,22 @@ def test_orthogonalize_refusals(lib):
     assert orth(lib, ns(), ws=FAKE + 16) == L.FPO_ERR_WORKSPACE
     need = lib.fpo_orthogonalize_workspace(C.byref(ns()), 1, i64(64), i64(128))
     assert need > 0 and orth(lib, ns(), ws_bytes=need - 1) == L.FPO_ERR_WORKSPACE
+
+
+def test_a_buffer_given_twice_is_refused(lib):
+    two = dict(n=2, rows=(64, 64), cols=(128, 128))
+    assert orth(lib, ns(), M=(FAKE, FAKE), O=(FAKE + 64, FAKE + 64), **two) == L.FPO_ERR_ARG
+    assert "same buffer" in lib.fpo_last_error().decode()
+    C2 = FAKE + 128
+    assert orth(lib, ns(), M=(C2, C2), O=(FAKE, FAKE + 64), ws=None, **two) == L.FPO_ERR_WORKSPACE  # M may repeat
+    assert orth(lib, ns(), M=(C2, FAKE), O=(FAKE, FAKE + 64), **two) == L.FPO_ERR_ARG
+    assert "is M of matrix 1" in lib.fpo_last_error().decode()
+    A, B = FAKE, FAKE + 64
+    for W, lp, st, want in (((A, A), (A, B), (A, B), L.FPO_ERR_ARG), ((A, B), (A, A), (A, B), L.FPO_ERR_ARG),
+                            ((A, B), (A, B), (B, B), L.FPO_ERR_ARG), ((A, B), (A, B), (A, B), L.FPO_ERR_WORKSPACE)):
+        u = L.UpdateBufs(ptrs(*W), ptrs(*lp), ptrs(*st), None, FAKE, None)
+        assert lib.fpo_muon_update(C.byref(muon()), 2, i64(64, 64), i64(128, 128), ptrs(A, A), FAKE, C.byref(u), None, 0,
+                                   None) == want
 
 
 def test_orthogonalize_workspace(lib):
