@@ -381,7 +381,7 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   double s = 0.0;
   for (int k = t; k < nblk; k += 256) s += part[k];
   s = sqrt(block_sum_d(s, red)) + a.eps;
-  const float f = s == 0.0 ? 0.f : (float)(pow2 / s);
+  const double f = s == 0.0 ? 0.0 : (double)pow2 / s;  // (double: beyond float's range for a norm under 2.4e-35)
   const T* x = (const T*)p.x[mat];
   const float* st = MUON ? p.state[mat] : nullptr;
   const Direction d = direction<MUON>(a, p, mat);
@@ -416,7 +416,8 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = st ? d.u(v[q], b[q]) : d.s * v[q];
       }
-      v *= f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = (float)((double)v[q] * f);
     }
     if (straight.hi) put(straight, r0 + r, c0 + c, ld_s, v);
     if (turned.hi) {

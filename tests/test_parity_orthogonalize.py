@@ -141,6 +141,16 @@ def test_orthogonalize_large(dev, rows, cols, n, dtype):
         assert off <= tol, f"matrix {i}: off by {off:.3e}, allowed {tol:.3e}"
 
 
+@pytest.mark.parametrize("scale", [1e-36, 1e37])
+def test_orthogonalize_extreme_norms(dev, scale):
+    """Norms whose reciprocal, or square, is beyond float32 (with eps 0)."""
+    M = (make((64, 72), "normal", 7, dev, F32) * scale).contiguous()
+    O = torch.empty_like(M)
+    api.fpo_orthogonalize([M], [O], eps=0.0)
+    E, tol = tolerance(host64(M) / scale, F32, eps=0.0)
+    assert np.linalg.norm(host64(O) - E) <= tol
+
+
 def test_orthogonalize_mixed_batch(dev):
     """Matrices of several sizes and both orientations in one call, one of them zero:
     each as if alone, and a call with the workspace of the first one kept is the same bit for bit."""
