@@ -73,6 +73,18 @@ def _stream(dev: torch.device) -> int:
     return torch.cuda.current_stream(dev).cuda_stream
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _call(dev: torch.device, f, *args) -> None:
+    """f(*args) with dev as the current device: stream handle 0 names the current device's."""
+    if dev.type != "cuda" or _current_device() == dev.index:
+        L.check(f(*args))
+    else:
+        with torch.cuda.device(dev):
+            L.check(f(*args))
+
+
 class _Keep:
     """Builds [host] pointer arrays and keeps them alive for one call."""
 
@@ -393,9 +405,8 @@ def fpo_orthogonalize(M, O, steps: int = 5, coefs=None, eps: float = 1e-7, ws=No
     lib = L.load()
     if ws is None:
         ws = workspace(lib.fpo_orthogonalize_workspace(C.byref(desc), n, rows, cols), dev)
-    L.check(lib.fpo_orthogonalize(C.byref(desc), n, rows, cols, k.arr(M, op, None, dev, n, "M"),
-                                  k.arr(O, op, lambda i: shapes[i], dev, n, "O"), _p(ws, None, None, dev, "ws"),
-                                  _nbytes(ws), _stream(dev)))
+    _call(dev, lib.fpo_orthogonalize, C.byref(desc), n, rows, cols, k.arr(M, op, None, dev, n, "M"),
+          k.arr(O, op, lambda i: shapes[i], dev, n, "O"), _p(ws, None, None, dev, "ws"), _nbytes(ws), _stream(dev))
     return ws
 
 
@@ -450,9 +461,8 @@ def fpo_muon_update(opt: MuonConfig, grad, W_master, state, W_sumsq=None, grad_s
     ub = L.UpdateBufs(k.arr(W_master, F32, shape, dev, n, "W_master"), k.arr(W_lp, dtype, shape, dev, n, "W_lp"),
                       k.arr(state, F32, shape, dev, n, "state"), None, _p(W_sumsq, F64, n, dev, "W_sumsq"),
                       _p(clip_scale, F32, n, dev, "clip_scale"))
-    L.check(lib.fpo_muon_update(C.byref(o), n, rows, cols, k.arr(grad, F32, None, dev, n, "grad"),
-                                _p(grad_sumsq, F64, n, dev, "grad_sumsq"), C.byref(ub), _p(ws, None, None, dev, "ws"),
-                                _nbytes(ws), _stream(dev)))
+    _call(dev, lib.fpo_muon_update, C.byref(o), n, rows, cols, k.arr(grad, F32, None, dev, n, "grad"),
+          _p(grad_sumsq, F64, n, dev, "grad_sumsq"), C.byref(ub), _p(ws, None, None, dev, "ws"), _nbytes(ws), _stream(dev))
     return ws
 
 
@@ -462,9 +472,9 @@ def fpo_layernorm(x, gain, bias, y, mean=None, rstd=None, eps=1e-5):
     T, d = x.shape
     op, dev = x.dtype, x.device
     desc = L.LnDesc(T, d, dtype_code(op), L.FPO_F32, eps, 0.0)
-    L.check(L.load().fpo_layernorm(
-        C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"), _p(bias, op, (d,), dev, "bias"),
-        _p(y, op, (T, d), dev, "y"), _p(mean, F32, (T,), dev, "mean"), _p(rstd, F32, (T,), dev, "rstd"), _stream(dev)))
+    _call(dev, L.load().fpo_layernorm, C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"),
+          _p(bias, op, (d,), dev, "bias"), _p(y, op, (T, d), dev, "y"), _p(mean, F32, (T,), dev, "mean"),
+          _p(rstd, F32, (T,), dev, "rstd"), _stream(dev))
 
 
 def fpo_layernorm_vjp_workspace(T: int, d: int) -> int:
@@ -482,8 +492,8 @@ def fpo_layernorm_vjp(x, gain, dy, dx=None, dx_lp=None, dgain=None, dbias=None, 
     lib = L.load()
     if ws is None:
         ws = workspace(lib.fpo_layernorm_vjp_workspace(C.byref(desc)), dev)
-    L.check(lib.fpo_layernorm_vjp(
-        C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"), _p(dy, dy.dtype, (T, d), dev, "dy"),
-        _p(dx, F32, (T, d), dev, "dx"), _p(dx_lp, op, (T, d), dev, "dx_lp"), _p(dgain, F32, (d,), dev, "dgain"),
-        _p(dbias, F32, (d,), dev, "dbias"), _p(ws, None, None, dev, "ws"), _nbytes(ws), _stream(dev)))
+    _call(dev, lib.fpo_layernorm_vjp, C.byref(desc), _p(x, op, (T, d), dev, "x"), _p(gain, op, (d,), dev, "gain"),
+          _p(dy, dy.dtype, (T, d), dev, "dy"), _p(dx, F32, (T, d), dev, "dx"), _p(dx_lp, op, (T, d), dev, "dx_lp"),
+          _p(dgain, F32, (d,), dev, "dgain"), _p(dbias, F32, (d,), dev, "dbias"), _p(ws, None, None, dev, "ws"),
+          _nbytes(ws), _stream(dev))
     return ws
