@@ -500,7 +500,7 @@ int each_ns_batch(int64_t n, const int64_t* rows, const int64_t* cols, F&& f) {
         ids[count++] = (int)j;
         done[j] = true;
       }
-    const int parts = (int)ceil_div(count, fpo::ns_batch_limit(s, l));
+    const int parts = (int)ceil_div(count, fpo::ns_batch_limit(s));
     for (int p = 0, at = 0; p < parts; ++p) {
       const int c = (count - at) / (parts - p);  // equal parts
       fpo::NsBatch b{};

@@ -369,8 +369,8 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsEw a, NsPtrs p) {
 
 // X = 2^e u / (||u|| + eps) as fp16 (PAIR: hi + lo), n x m and padded with zeros, and X^T
 // where it is wanted (XT.hi: small products, both then in their layout); one 64 x 64 tile
-// a workgroup. The matrix that is laid out
-// like the source (X, or X^T of a tall one) is stored as read, the other through LDS.
+// a workgroup. The matrix that is laid out like the source (X, or X^T of a tall one) is
+// stored as read, the other through LDS.
 template <typename T, bool MUON, bool PAIR>
 __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat X, NsMat XT, float pow2, int nblk) {
   __shared__ float tile[kNsEdge][kNsEdge + 1];

@@ -251,10 +251,9 @@ struct NsLaunch {
 
 // Matrices of one batch at most. A batch's smallest launches (n x n, tiles on and under
 // the diagonal) should fill the CUs several times; a larger one only costs workspace.
-inline int ns_batch_limit(int64_t n, int64_t m) {
+inline int ns_batch_limit(int64_t n) {
   const int64_t t = ceil_div(n, 256), tri = t * (t + 1) / 2;
   const int64_t want = ceil_div(8 * kCus, tri);
-  (void)m;
   return (int)std::min<int64_t>(kMaxMats, std::max<int64_t>(want, 4));
 }
 

@@ -70,7 +70,6 @@ struct NsFinish {
   int mp;                    // X's row pitch
   uint64_t tall;
   float pow2;                // 2^-e of X
-  int lp_bf16;
   // muon
   float decay, lr_wd;        // 1 - lr weight_decay, lr weight_decay
   float step[2];             // lr times the scale of O, by orientation

@@ -134,6 +134,40 @@ def test_vjp_many_rows(dev):
         run_vjp(dev, T, d, BF, F32)
 
 
+def test_offsets_past_32_bits(dev):
+    """More than 2^31 elements; the first and last rows against the oracle, the parameter
+    gradients against float64 sums over all of them."""
+    T, d = (1 << 19) + 77, 4104
+    g = torch.Generator(device=dev)
+    g.manual_seed(3)
+    x = torch.empty(T, d, device=dev, dtype=BF).normal_(generator=g)
+    dy = torch.empty(T, d, device=dev, dtype=BF).normal_(generator=g)
+    gain = rows(1, d, dev, BF, 4)[0]
+    y, dx_lp = torch.empty_like(x), torch.empty_like(x)
+    dgain, dbias = torch.empty(d, device=dev), torch.empty(d, device=dev)
+    api.fpo_layernorm(x, gain, None, y)
+    api.fpo_layernorm_vjp(x, gain, dy, dx_lp=dx_lp, dgain=dgain, dbias=dbias)
+    for part in (slice(0, 3), slice(T // 2, T // 2 + 3), slice(T - 3, T)):
+        xs, ds = host64(x[part]), host64(dy[part])
+        Y, _, _, ty = forward_tol(xs, host64(gain), None, 1e-5)
+        check("y", y[part], Y, ty, BF)
+        dx, _, _, tdx, _, _ = vjp_tol(xs, host64(gain), ds, 1e-5, 0.0, 3)
+        check("dx_lp", dx_lp[part], dx, tdx, BF)
+    wg, wb, ag, ab, size = [torch.zeros(d, device=dev, dtype=torch.float64) for _ in range(5)]
+    for i in range(0, T, 1 << 15):
+        xs, ds = x[i:i + (1 << 15)].double(), dy[i:i + (1 << 15)].double()
+        xc = xs - xs.mean(1, keepdim=True)
+        rstd = 1 / (xc.square().mean(1, keepdim=True) + 1e-5).sqrt()
+        wg += (ds * xc * rstd).sum(0)
+        wb += ds.sum(0)
+        ag += (ds * xc * rstd).abs().sum(0)
+        ab += ds.abs().sum(0)
+        size += (ds.abs() * (xs.abs() + xs.abs().mean(1, keepdim=True)) * rstd).sum(0)
+    r = (T // 256 + 5) * U  # (rows of this length run on 256 workgroups at least)
+    assert ((dgain - wg).abs() <= r * ag + 2 * n_round(d) * U * size).all()
+    assert ((dbias - wb).abs() <= r * ab).all()
+
+
 def test_vjp_floor(dev):
     """Rows under, around and over the floor."""
     T, d = 64, 1032

@@ -151,6 +151,41 @@ def test_orthogonalize_extreme_norms(dev, scale):
     assert np.linalg.norm(host64(O) - E) <= tol
 
 
+@pytest.mark.parametrize("rows,cols,dtype", [(16384, 32768, BF), (32760, 16376, BF), (64, 1 << 23, BF),
+                                             (8192, 32768, F32)])
+def test_orthogonalize_largest(dev, rows, cols, dtype):
+    """2^29 entries (float32: 2^28). One entry a row (and at most one a column), so that
+    each is mapped by itself and every other entry is zero: p(p(...(s / ||M||))).
+
+    Tolerance, relative by entry. FPO_BF16: X is rounded to fp16 before each of at most
+    five groups, 2^-11, and |s p'/p| of a later step is 2 at most, of one with small s 1
+    at most: 9 x 2^-11 with the last groups' 4, 2 and 1 and two early ones; O is rounded by
+    2^-8. FPO_F32: the same nine times for X's rounding and products, 3 x 2^-22 each, and
+    2^-24, the diagonals' cancellation (4.775 of 0.68) eight times as much: under 2^-13."""
+    n = min(rows, cols)
+    g = torch.Generator(device=dev)
+    g.manual_seed(n)
+    longer = max(rows, cols)
+    at = 1 + torch.randperm(longer - 2, generator=g, device=dev)[:n]
+    at[0], at[-1] = 0, longer - 1  # the corners
+    v = (0.5 + 1.5 * torch.rand(n, generator=g, device=dev)).to(dtype)
+    v[::2] *= -1
+    M = torch.zeros(rows, cols, device=dev, dtype=dtype)
+    i = torch.arange(n, device=dev)
+    where = (i, at) if rows <= cols else (at, i)
+    M[where] = v
+    O = torch.full_like(M, float("nan"))
+    api.fpo_orthogonalize([M], [O])
+    s = v.double()
+    s = s / (s.square().sum().sqrt() + 1e-7)
+    a, b, c = P.MUON_COEF
+    for _ in range(5):
+        s = a * s + b * s ** 3 + c * s ** 5
+    off = ((O[where].double() - s) / s).abs().max().item()
+    assert off <= (2 ** -8 + 9 * 2 ** -11 if dtype == BF else 2 ** -13)
+    assert int((O != 0).sum()) == n
+
+
 def test_orthogonalize_mixed_batch(dev):
     """Matrices of several sizes and both orientations in one call, one of them zero:
     each as if alone, and a call with the workspace of the first one kept is the same bit for bit."""
