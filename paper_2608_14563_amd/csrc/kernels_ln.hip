@@ -8,8 +8,8 @@
 // reductions over the lanes that share it (the squares are of differences from the
 // mean, so that a large mean costs no digits), and everything else is elementwise.
 //
-// A row is shared by 64 lanes (d up to 1024 or 2048), 256 (up to 4096), 512 (8192) or 1024
-// (16384), each holding up to four chunks of eight neighbouring elements; longer rows are
+// A row is shared by 16 lanes (d up to 128), 32 (256), 64 (1024 or 2048), 256 (up to 4096),
+// 512 (8192) or 1024 (16384), each holding up to four chunks of eight neighbouring elements; longer rows are
 // read again for every reduction. A workgroup takes every grid-th row, loading the next
 // one before the current one's reductions, and keeps gain (and bias) in registers (8192 x
 // 4096 bf16 forward 32 -> 27 us, 5.0 TB/s: they were as many bytes from L2 as x and y). In
@@ -62,19 +62,19 @@ __device__ __forceinline__ float sum8(f32x8 v) {
   return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
 
-// Sum over the LANES lanes of a row; 64 lanes: within the wave, else the workgroup is one
+// Sum over the LANES lanes of a row; up to 64: within the wave, else the workgroup is one
 // row's. `red` holds 3 x 16 floats.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float* red) {
-  if constexpr (LANES == 64) return wave_sum(v);
+  if constexpr (LANES <= 64) return wave_sum<LANES>(v);
   else return block_sum(v, red);
 }
 // Three of them in one exchange.
 template <int LANES>
 __device__ __forceinline__ void row_sum3(float& a, float& b, float& c, float* red) {
-  a = wave_sum(a);
-  b = wave_sum(b);
-  c = wave_sum(c);
+  a = wave_sum<std::min(LANES, 64)>(a);
+  b = wave_sum<std::min(LANES, 64)>(b);
+  c = wave_sum<std::min(LANES, 64)>(c);
   if constexpr (LANES > 64) {
     const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
     __syncthreads();
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_forward_kernel(const T* 
         if (bias) rb[k].load(bias + 8 * (lane + k * LANES));
       }
   }
-  // (with several slots a row's lanes are a whole wave, and nothing in the loop is a barrier)
+  // (with several slots a row's lanes are in one wave, and nothing in the loop is a barrier)
   for (; row < rows; row += step) {
     f32x8 v[NR];
     float s = 0.f;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
   if constexpr (AHEAD) {
     if (row < a.rows) fetch(row);
   }
-  // with several slots a row's lanes are whole waves and nothing in the loop is a barrier
+  // with several slots a row's lanes are in one wave and nothing in the loop is a barrier
   for (; row < a.rows; row += step) {
     f32x8 vx[NR], vd[NR];
     auto each = [&](auto&& f) {  // f(chunk, k, x, dy, gain)
@@ -329,8 +329,8 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
           if (a.pgain) store8(a.pgain + at, pg[k]);
           if (a.pbias) store8(a.pbias + at, pb[k]);
         }
-    } else {  // the four waves' sums, in a fixed order
-      __shared__ f32x8 part[SLOTS][64];
+    } else {  // the slots' sums, in a fixed order
+      __shared__ f32x8 part[SLOTS][LANES];
 #pragma unroll
       for (int k = 0; k < NR; ++k)
 #pragma unroll
@@ -339,11 +339,11 @@ __global__ __launch_bounds__(ln_threads(LANES)) void ln_vjp_kernel(LnVjp a) {
           part[slot][lane] = which ? pb[k] : pg[k];
           __syncthreads();
           float* out = which ? a.pbias : a.pgain;
-          if (slot == 0 && out && lane + k * 64 < nc) {
+          if (slot == 0 && out && lane + k * LANES < nc) {
             f32x8 t = part[0][lane];
 #pragma unroll
             for (int w = 1; w < SLOTS; ++w) t += part[w][lane];
-            store8(out + (int64_t)blockIdx.x * d + 8 * (lane + k * 64), t);
+            store8(out + (int64_t)blockIdx.x * d + 8 * (lane + k * LANES), t);
           }
         }
     }
@@ -387,6 +387,8 @@ constexpr int kLnBlocks = 2048;              // workgroups of the VJP without pa
 struct LnShape {
   int lanes, nv;
 };
+// Rows of up to 256 elements, as norms of single heads have them, share a wave (2^20 x 128
+// bf16: forward 318 -> 107 us, VJP 617 -> 192 us, 4.9 and 5.5 TB/s).
 // Rows too few for four of them to a workgroup on every CU have a workgroup each. Between
 // 1032 and 2048 elements a wave a row is quicker in the forward pass (16384 x 2048: 26 us
 // against 33 with 256 lanes) and slower in the VJP, whose sums then leave one wave a SIMD
@@ -394,6 +396,8 @@ struct LnShape {
 LnShape ln_shape(int64_t T, int64_t d, bool vjp) {
   const int64_t nc = d / 8;
   const bool few = T < 4 * kCus;
+  if (nc <= 16) return {16, 1};
+  if (nc <= 32) return {32, 1};
   if (nc <= 64) return {64, 1};
   if (nc <= 128) return few ? LnShape{256, 1} : LnShape{64, 2};
   if (nc <= 256) return few || vjp ? LnShape{256, 1} : LnShape{64, 4};
@@ -406,7 +410,9 @@ LnShape ln_shape(int64_t T, int64_t d, bool vjp) {
 // f(std::integral_constant lanes, nv) for the shape
 template <class F>
 void with_shape(LnShape s, F&& f) {
-  if (s.lanes == 64 && s.nv == 1) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  if (s.lanes == 16) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  else if (s.lanes == 32) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+  else if (s.lanes == 64 && s.nv == 1) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
   else if (s.lanes == 64 && s.nv == 2) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
   else if (s.lanes == 64) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 4>{});
   else if (s.lanes == 256 && s.nv == 1) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
@@ -471,7 +477,7 @@ int ln_vjp_blocks(int64_t T, int64_t d) {
   const LnShape s = ln_shape(T, d, true);
   // about as many workgroups a CU as their registers let run at once; another one more has
   // another row of partials to write and read
-  const int per_cu = s.lanes == 64 ? 2 : s.lanes == 256 ? (s.nv == 1 ? 3 : 2) : 1;
+  const int per_cu = s.lanes <= 64 ? 2 : s.lanes == 256 ? (s.nv == 1 ? 3 : 2) : 1;
   return (int)std::min<int64_t>(ceil_div(T, ln_threads(s.lanes) / s.lanes), kCus * per_cu);
 }
 
