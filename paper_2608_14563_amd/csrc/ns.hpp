@@ -156,7 +156,7 @@ inline NsSplit ns_split(int64_t M, int64_t N, int64_t K, int64_t mats, bool symm
   const double kt = (double)ceil_div(K, 64);
   // (as in big_tiles, with this epilogue: stored twice, operands read again)
   auto big = [&](int64_t n) { return n ? (1.0 + 0.6 * (double)n / kCus) * kt + 20.0 : 0.0; };
-  auto quarters = [&](int64_t n) { return (double)ceil_div(n, kCus) * (0.45 * kt + 11.5); };
+  auto quarters = [&](int64_t n) { return (double)ceil_div(n, kCus) * (0.45 * kt + 8.0); };
   const int64_t n = mats * ns_tiles(M, N, 256, symmetric), rem = n % kCus, whole = n - rem;
   const double waves = (double)(n / kCus) * big(kCus);
   NsSplit best{n, waves + big(rem)};
@@ -171,10 +171,10 @@ inline NsSplit ns_split(int64_t M, int64_t N, int64_t K, int64_t mats, bool symm
 // large ones, and the number of steps in the first group (ns_plan), by the least estimated
 // time of the products of five steps.
 //  * Up to 256 small tiles take 4.2 us and 4.3 ns a K entry (pairs 4.6 and 9.5), more of
-//    them 4.6 us and, per 256, 3.6 us and 2.1 ns a K entry (6 and 5.5). Measured, us small /
-//    large: fp16, 64 x 168 81 / 162, 512 x 1376 128 / 270, eight of them 242 / 313, 1024 x
-//    1024 158 / 310, eight 557 / 547, three 1280 x 3456 537 / 486. Pairs, 256 x 688 140 /
-//    271, eight 512 x 1376 402 / 474, three 1280 x 3456 1153 / 972.
+//    them 4.6 us and, per 256, 3.6 us and 2.7 ns a K entry (5 and 6.5). Measured, us small /
+//    large: fp16, 64 x 168 75 / 116, 512 x 1376 125 / 199, eight of them 242 / 239, 1024 x
+//    1024 137 / 238, eight 444 / 477, three 1536 x 4144 820 / 553. Pairs, 256 x 688 129 /
+//    240, eight 512 x 1376 394 / 418, three 1536 x 4144 1810 / 1435.
 //  * One step a group takes three launches a step (15), groups of 2, 1, 2 take 17: fewer
 //    where a launch's latency is what counts.
 //  * Three steps in the first group of the large tiles: see ns_plan.
@@ -184,7 +184,7 @@ struct NsChoice {
 };
 inline double ns_small_us(int64_t tiles, int64_t K, bool bf16) {
   if (tiles <= kCus) return bf16 ? 4.2 + 0.0043 * (double)K : 4.6 + 0.0095 * (double)K;
-  return 4.6 + (double)tiles / kCus * (bf16 ? 3.6 + 0.0021 * (double)K : 6.0 + 0.0055 * (double)K);
+  return 4.6 + (double)tiles / kCus * (bf16 ? 3.6 + 0.0027 * (double)K : 5.0 + 0.0065 * (double)K);
 }
 inline NsChoice ns_choose(int64_t n, int64_t m, int count, bool bf16) {
   const int64_t np = ceil_div(n, 64) * 64, mp = ceil_div(m, 64) * 64;
