@@ -505,7 +505,7 @@ int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, cons
  *   dy           [T, d] (dy_dtype): e.g. fpo_output_error's g_pre
  *   dx           float [T, d] out, nullable;  dx_lp [T, d] (dtype) out, nullable: dx rounded once
  *   dgain, dbias float [d] out, each nullable; sums in a fixed order
- * At least one output is required.
+ * At least one output is required; none may overlap an input or another output.
  * Returns FPO_OK or an fpo_status. */
 size_t fpo_layernorm_vjp_workspace(const fpo_ln_desc* desc);
 int fpo_layernorm_vjp(const fpo_ln_desc* desc, const void* x, const void* gain, const void* dy, float* dx,

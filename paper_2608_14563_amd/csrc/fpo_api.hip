@@ -1020,6 +1020,7 @@ int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, cons
   if (!x || !y) return fail(FPO_ERR_NULL, "fpo_layernorm: x and y are required");
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gain, 16) || !aligned(bias, 16))
     return fail(FPO_ERR_ARG, "fpo_layernorm: tensors must be 16-byte aligned");
+  if (y == x) return fail(FPO_ERR_ARG, "fpo_layernorm: y is x");
   fpo::LnLaunch L{};
   L.bf16 = desc->dtype == FPO_BF16;
   L.T = desc->T;
@@ -1049,6 +1050,14 @@ int fpo_layernorm_vjp(const fpo_ln_desc* desc, const void* x, const void* gain, 
   if (!dx && !dx_lp && !dgain && !dbias) return fail(FPO_ERR_NULL, "fpo_layernorm_vjp: no output is asked for");
   for (const void* p : {x, gain, dy, (const void*)dx, (const void*)dx_lp, (const void*)dgain, (const void*)dbias})
     if (!aligned(p, 16)) return fail(FPO_ERR_ARG, "fpo_layernorm_vjp: tensors must be 16-byte aligned");
+  const void* const outs[4] = {dx, dx_lp, dgain, dbias};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    if (outs[i] == x || outs[i] == dy || outs[i] == gain)
+      return fail(FPO_ERR_ARG, "fpo_layernorm_vjp: an output is one of the inputs");
+    for (int j = 0; j < i; ++j)
+      if (outs[i] == outs[j]) return fail(FPO_ERR_ARG, "fpo_layernorm_vjp: two outputs are the same buffer");
+  }
   if (dgain || dbias)
     if (int e = check_ws(ws, ws_bytes, ln_vjp_ws(*desc), "fpo_layernorm_vjp")) return e;
   fpo::LnLaunch L{};

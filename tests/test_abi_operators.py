@@ -148,10 +148,11 @@ def ln(T=4, d=64, dtype=L.FPO_BF16, dy=L.FPO_F32, eps=1e-5, min_std=0.0):
 
 
 def test_layernorm_refusals(lib):
-    def fwd(desc, x=FAKE, gain=FAKE, bias=FAKE, y=FAKE):
+    def fwd(desc, x=FAKE, gain=FAKE, bias=FAKE, y=FAKE + 256):
         return lib.fpo_layernorm(C.byref(desc) if desc else None, x, gain, bias, y, None, None, None)
 
-    def vjp(desc, x=FAKE, gain=FAKE, dy=FAKE, dx=FAKE, lp=FAKE, dg=FAKE, db=FAKE, ws=FAKE, ws_bytes=1 << 40):
+    def vjp(desc, x=FAKE, gain=FAKE, dy=FAKE, dx=FAKE + 256, lp=FAKE + 512, dg=FAKE + 768, db=FAKE + 1024, ws=FAKE,
+            ws_bytes=1 << 40):
         return lib.fpo_layernorm_vjp(C.byref(desc) if desc else None, x, gain, dy, dx, lp, dg, db, ws, ws_bytes, None)
 
     for f in (fwd, vjp):
@@ -171,6 +172,11 @@ def test_layernorm_refusals(lib):
     assert vjp(ln(), dx=None, lp=None, dg=None, db=None) == L.FPO_ERR_NULL
     for k in ("dx", "lp", "dg", "db"):
         assert vjp(ln(), **{k: FAKE + 4}) == L.FPO_ERR_ARG
+    assert fwd(ln(), y=FAKE) == L.FPO_ERR_ARG
+    for k in ("dx", "lp", "dg", "db"):
+        assert vjp(ln(T=600), **{k: FAKE}) == L.FPO_ERR_ARG
+        assert "one of the inputs" in lib.fpo_last_error().decode()
+    assert vjp(ln(T=600), lp=FAKE + 256) == L.FPO_ERR_ARG and vjp(ln(T=600), db=FAKE + 768) == L.FPO_ERR_ARG
     assert vjp(ln(T=600), ws=None) == L.FPO_ERR_WORKSPACE
     assert vjp(ln(T=600), ws_bytes=16) == L.FPO_ERR_WORKSPACE
     assert vjp(ln(T=600), ws=FAKE + 4) == L.FPO_ERR_WORKSPACE

@@ -10,6 +10,8 @@ and the orthogonalised direction may be off by 2% (fp16 products of a gradient o
 tokens, whose rank is under the matrix's: twice what one fp16 rounding a matrix costs is
 1.5%, and 2^-8); the step it scales is 1% of W, three steps 3 x 2e-2 x 1e-2. FPO_F32:
 products to 2^-22, the direction to 1e-4 for the same reason."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -117,3 +119,76 @@ def test_captured_step_replays_match_eager(dev):
         torch.cuda.synchronize()
         for k in ("y", "dx", "dgain", "dbias", "dW", "W", "W_lp", "mom", "gain", "bias", "W_sumsq", "p_sumsq"):
             assert torch.equal(eager[k], graphed[k]), k
+
+
+OUT = ("y", "dx", "dx_lp", "dgain", "dbias", "dW", "W", "W_lp", "mom", "gain", "bias", "W_sumsq", "p_sumsq", "clip")
+
+
+def test_two_threads_two_streams(dev):
+    """Two host threads, each on its own stream with its own buffers, as if each were alone."""
+    ref = [make(dev, torch.bfloat16, seed) for seed in (1, 2)]
+    for s in ref:
+        for k in (1, 2, 3):
+            step(s, k, torch.bfloat16)
+    got = [make(dev, torch.bfloat16, seed) for seed in (1, 2)]
+    torch.cuda.synchronize()
+    errors = []
+
+    def run(s):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for k in (1, 2, 3):
+                    step(s, k, torch.bfloat16)
+            st.synchronize()
+        except Exception as e:  # pragma: no cover - reported below
+            errors.append(e)
+
+    threads = [threading.Thread(target=run, args=(s,)) for s in got]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for r, s in zip(ref, got):
+        for k in OUT:
+            assert torch.equal(r[k], s[k]), k
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_large_tiles_captured_and_replayed(dev, dtype):
+    """The Muon step on sizes that take the large tiles, whole and in quarters, and on small
+    ones beside them: eager twice and captured, the same bits."""
+    shapes = [(2048, 2560)] * 4 + [(2560, 2048)] * 4 + [(72, 200), (1288, 1544)]
+    g = torch.Generator(device=dev)
+
+    def state():
+        g.manual_seed(5)
+        r = lambda s: torch.randn(*s, generator=g, device=dev)  # noqa: E731
+        return dict(grad=[r(x) for x in shapes], W=[0.02 * r(x) for x in shapes], state=[r(x) for x in shapes],
+                    W_lp=[torch.empty(*x, device=dev, dtype=dtype) for x in shapes],
+                    sumsq=torch.ones(len(shapes), device=dev, dtype=torch.float64),
+                    ws=api.workspace(api.fpo_muon_update_workspace(shapes, dtype), dev))
+
+    def run(s):
+        api.fpo_muon_update(api.MuonConfig(lr=1e-2, clip_frac=0.0, step=2), s["grad"], s["W"], s["state"],
+                            W_sumsq=s["sumsq"], W_lp=s["W_lp"], dtype=dtype, ws=s["ws"])
+
+    eager, again, graphed = state(), state(), state()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        run(graphed)
+    for _ in range(3):
+        run(eager)
+        run(again)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for s in (again, graphed):
+            assert torch.equal(eager["sumsq"], s["sumsq"])
+            for k in ("W", "state", "W_lp"):
+                assert all(torch.equal(a, b) for a, b in zip(eager[k], s[k])), k
+    for W, q, lp in zip(eager["W"], eager["sumsq"].tolist(), eager["W_lp"]):
+        assert torch.isfinite(W).all() and torch.equal(lp, W.to(dtype))
+        assert abs(q / W.double().square().sum().item() - 1) < 1e-12
