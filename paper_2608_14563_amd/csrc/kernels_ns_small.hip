@@ -50,7 +50,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
   constexpr bool SYM = WHAT != kApplyX, LAST = !std::is_same<Last, NsNotLast>::value;
   constexpr int U = (NW == 4 ? 2 : 4) / (PAIR ? 2 : 1);  // K steps loaded together
   constexpr int E = 8 / NW, H = NW / 2;           // chunks of eight entries a thread stores; partial sums in LDS
-  __shared__ float red[H][kSmallEdge][kRedLd];
+  __shared__ __align__(16) float red[H][kSmallEdge][kRedLd];
   const int ntm = g.M / kSmallEdge;
   int mat = blockIdx.x / g.tiles;
   const int loc = (int)blockIdx.x - mat * g.tiles;
@@ -94,8 +94,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
   if constexpr (WHAT != kGram && !PAIR) adv = a.diag[mat * a.dstride + row];
   // ---- the wave's share of K
   const int steps = g.K / 16;
-  const uint16_t* ap = ah + (int64_t)m0 * g.K + 8 * l;
-  const uint16_t* bp = bh + (int64_t)n0 * g.K + 8 * l;
+  const uint16_t* ap = ah + (int64_t)m0 * g.K;
+  const uint16_t* bp = bh + (int64_t)n0 * g.K;
   const int64_t r32 = (int64_t)32 * g.K;  // the next 32 rows
   f32x16 acc[2][2] = {{f32x16{}, f32x16{}}, {f32x16{}, f32x16{}}};
   auto load = [&](SmallFrag<PAIR> (&f)[U], int s0) {
@@ -107,11 +107,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
       const uint16_t* pb = bp + 512 * (int64_t)s;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        f[u].a[h] = *reinterpret_cast<const u32x4*>(pa + h * r32);
-        f[u].b[h] = *reinterpret_cast<const u32x4*>(pb + h * r32);
+        f[u].a[h] = reinterpret_cast<const u32x4*>(pa + h * r32)[l];
+        f[u].b[h] = reinterpret_cast<const u32x4*>(pb + h * r32)[l];
         if constexpr (PAIR) {
-          f[u].al[h] = *reinterpret_cast<const u32x4*>(pa + h * r32 + a.lo_off);
-          f[u].bl[h] = *reinterpret_cast<const u32x4*>(pb + h * r32 + b.lo_off);
+          f[u].al[h] = reinterpret_cast<const u32x4*>(pa + h * r32 + a.lo_off)[l];
+          f[u].bl[h] = reinterpret_cast<const u32x4*>(pb + h * r32 + b.lo_off)[l];
         }
       }
     }
@@ -124,10 +124,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          acc[h][i] = mfma_16bit<true>(f[u].a[h], f[u].b[i], acc[h][i]);
+          acc[h][i] = mfma_16bit<true>(f[u].b[i], f[u].a[h], acc[h][i]);
           if constexpr (PAIR) {
-            acc[h][i] = mfma_16bit<true>(f[u].a[h], f[u].bl[i], acc[h][i]);
-            acc[h][i] = mfma_16bit<true>(f[u].al[h], f[u].b[i], acc[h][i]);
+            acc[h][i] = mfma_16bit<true>(f[u].bl[i], f[u].a[h], acc[h][i]);
+            acc[h][i] = mfma_16bit<true>(f[u].b[i], f[u].al[h], acc[h][i]);
           }
         }
     }
@@ -142,19 +142,22 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
     multiply(f1, s + kAhead);
   }
   // ---- sums: the upper half of the waves into LDS, the lower half adds its own, and the
-  // H sums are added below
-  const int lr = 4 * (l >> 5), lc = l & 31;
+  // H sums are added below. (The products are taken as B A^T, so that a lane has four
+  // neighbouring columns of a row.)
+  const int lr = l & 31, lc = 4 * (l >> 5);
   auto each = [&](auto&& f) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) f(acc[h][i][r], red[w % H][32 * h + 8 * (r >> 2) + lr + (r & 3)][32 * i + lc]);
+        for (int r = 0; r < 16; r += 4)
+          f(f32x4{acc[h][i][r], acc[h][i][r + 1], acc[h][i][r + 2], acc[h][i][r + 3]},
+            *reinterpret_cast<f32x4*>(&red[w % H][32 * h + lr][32 * i + 2 * r + lc]));
   };
-  if (w >= H) each([](float v, float& m) { m = v; });
+  if (w >= H) each([](f32x4 v, f32x4& m) { m = v; });
   __syncthreads();
-  if (w < H) each([](float v, float& m) { m += v; });
+  if (w < H) each([](f32x4 v, f32x4& m) { m += v; });
   __syncthreads();
   // ---- epilogue
   const float alpha = set ? g.alpha[1] : g.alpha[0];
