@@ -52,10 +52,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
   constexpr int E = 8 / NW, H = NW / 2;           // chunks of eight entries a thread stores; partial sums in LDS
   __shared__ __align__(16) float red[H][kSmallEdge][kRedLd];
   const int ntm = g.M / kSmallEdge;
-  int mat = blockIdx.x / g.tiles;
-  const int loc = (int)blockIdx.x - mat * g.tiles;
-  const int set = mat / g.count;
-  mat -= set * g.count;
+  const int loc = blockIdx.x, mat = blockIdx.y, set = blockIdx.z;
   int tm, tn;
   if constexpr (SYM) {
     tri_tile(loc, ntm, tm, tn);
@@ -268,20 +265,21 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
 }
 
 template <int WHAT, class Last>
-void launch_small(const char* name, const NsGemmArgs& g, int64_t grid, bool pair, const NsMat& x_of_b,
+void launch_small(const char* name, const NsGemmArgs& g, int sets, bool pair, const NsMat& x_of_b,
                   const NsMat& to_t, int rows, const Last& last, hipStream_t st) {
+  const dim3 grid((unsigned)g.tiles, (unsigned)g.count, (unsigned)sets);
   auto waves = [&](auto nw) {
     constexpr int NW = decltype(nw)::value;
     if (pair)
       FPO_LAUNCH(name, st,
-                 (ns_small_kernel<WHAT, true, NW, Last><<<dim3((unsigned)grid), dim3(64 * NW), 0, st>>>(
+                 (ns_small_kernel<WHAT, true, NW, Last><<<grid, dim3(64 * NW), 0, st>>>(
                      g, x_of_b, to_t, rows, last)));
     else
       FPO_LAUNCH(name, st,
-                 (ns_small_kernel<WHAT, false, NW, Last><<<dim3((unsigned)grid), dim3(64 * NW), 0, st>>>(
+                 (ns_small_kernel<WHAT, false, NW, Last><<<grid, dim3(64 * NW), 0, st>>>(
                      g, x_of_b, to_t, rows, last)));
   };
-  if (grid <= kCus) waves(std::integral_constant<int, 8>{});
+  if ((int64_t)g.tiles * g.count * sets <= kCus) waves(std::integral_constant<int, 8>{});
   else waves(std::integral_constant<int, 4>{});
 }
 
@@ -290,15 +288,14 @@ void launch_small(const char* name, const NsGemmArgs& g, int64_t grid, bool pair
 hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
                                 const NsMat& to_t, bool rows, const NsLast* last, hipStream_t st) {
   g.tiles = (int)ns_tiles(g.M, g.N, kSmallEdge, what != kApplyX);
-  const int64_t grid = (int64_t)g.tiles * g.count * sets;
   const NsNotLast no;
   switch (what) {
-    case kGram: launch_small<kGram>(name, g, grid, pair, x_of_b, to_t, 0, no, st); break;
-    case kMul: launch_small<kMul>(name, g, grid, pair, x_of_b, to_t, 0, no, st); break;
-    case kPoly: launch_small<kPoly>(name, g, grid, pair, x_of_b, to_t, 0, no, st); break;
+    case kGram: launch_small<kGram>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
+    case kMul: launch_small<kMul>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
+    case kPoly: launch_small<kPoly>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
     default:
-      if (last) launch_small<kApplyX>(name, g, grid, pair, x_of_b, to_t, 0, *last, st);
-      else launch_small<kApplyX>(name, g, grid, pair, x_of_b, to_t, rows, no, st);
+      if (last) launch_small<kApplyX>(name, g, sets, pair, x_of_b, to_t, 0, *last, st);
+      else launch_small<kApplyX>(name, g, sets, pair, x_of_b, to_t, rows, no, st);
       break;
   }
   return hipGetLastError();

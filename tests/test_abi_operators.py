@@ -300,3 +300,30 @@ def test_bounds_and_exponents(host):
                     assert np.abs(v).max() * 2.0 ** e <= 2 ** 13
                 lam = lam * B * B
         assert np.sqrt(lam).max() * 2.0 ** e_out <= 2 ** 13
+
+
+def test_call_makes_the_tensors_device_current(monkeypatch):
+    import torch
+
+    from paper_2608_14563_amd import api
+    seen = []
+
+    class Device:
+        def __init__(self, d):
+            self.d = d
+
+        def __enter__(self):
+            seen.append(("enter", self.d))
+
+        def __exit__(self, *a):
+            seen.append("exit")
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(api, "_current_device", lambda: 0)
+    here, there = torch.device("cuda", 0), torch.device("cuda", 1)
+    api._call(here, lambda x: seen.append(x) or 0, 5)
+    assert seen == [5]
+    api._call(there, lambda x: seen.append(x) or 0, 6)
+    assert seen == [5, ("enter", there), 6, "exit"]
+    with pytest.raises(L.FpoError):
+        api._call(here, lambda: L.FPO_ERR_ARG)
