@@ -414,8 +414,8 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A,
  * products to about fp32 precision (pairs of fp16, three products).
  * A matrix of zeros gives zeros (with eps 0 too). Non-finite entries give a matrix
  * of unspecified values; the other matrices of the call are not affected. Singular
- * values below about 1e-6 of the norm (fp32: 1e-7) carry rounding noise, enlarged as
- * they are (3.4445 times a step).
+ * values below about 4e-5 of the norm (the size of what rounding a matrix to bf16 adds;
+ * fp32: 1e-7) carry rounding noise, enlarged as they are (3.4445 times a step).
  * coef  [host] 3 * steps doubles (a, b, c of each step), NULL: the defaults. They are
  *       refused (FPO_ERR_ARG) if they let a singular value in [0, 1] grow past 1024
  *       in any step.
