@@ -509,11 +509,6 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   __shared__ double red[4];
   const int mat = blockIdx.z, t = threadIdx.x;
   const int i0 = blockIdx.y * kNsEdge, j0 = blockIdx.x * kNsEdge;  // rows and columns of X
-  const double* part = a.part + (int64_t)mat * kNsNormBlocks;
-  double s = 0.0;
-  for (int k = t; k < nblk; k += 256) s += part[k];
-  s = sqrt(block_sum_d(s, red)) + a.eps;
-  const double f = s == 0.0 ? 0.0 : (double)pow2 / s;  // (double: beyond float's range for a norm under 2.4e-35)
   const T* x = (const T*)p.x[mat];
   const float* st = MUON ? p.state[mat] : nullptr;
   const Direction d = direction<MUON>(a, p, mat);
@@ -521,6 +516,24 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   // source rows and columns of this tile
   const int R = tall ? a.cols_m : a.rows_n, C = tall ? a.rows_n : a.cols_m;
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
+  // loaded ahead of the norm, which waits for the partials and the workgroup
+  f32x4 v[4], b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = k * 16 + (t >> 4), c = 4 * (t & 15);
+    v[k] = b[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (r0 + r < R && c0 + c < C) {  // C is a multiple of 8
+      const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
+      v[k] = ld4<T>(x, at);
+      if constexpr (MUON)
+        if (st) b[k] = ld4<float>(st, at);
+    }
+  }
+  const double* part = a.part + (int64_t)mat * kNsNormBlocks;
+  double s = 0.0;
+  for (int k = t; k < nblk; k += 256) s += part[k];
+  s = sqrt(block_sum_d(s, red)) + a.eps;
+  const double f = s == 0.0 ? 0.0 : (double)pow2 / s;  // (double: beyond float's range for a norm under 2.4e-35)
   const NsMat straight = tall ? XT : X, turned = tall ? X : XT;
   const int ld_s = tall ? a.np : a.mp, ld_t = tall ? a.mp : a.np;
   auto put = [&](const NsMat& to, int i, int j, int ld, f32x4 v) {
@@ -539,22 +552,17 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int r = k * 16 + (t >> 4), c = 4 * (t & 15);
-    f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (r0 + r < R && c0 + c < C) {  // C is a multiple of 8
-      const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
-      v = ld4<T>(x, at);
-      if constexpr (MUON) {
-        const f32x4 b = st ? ld4<float>(st, at) : v;
+    f32x4 u = v[k];
+    if constexpr (MUON) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = st ? d.u(v[q], b[q]) : d.s * v[q];
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = (float)((double)v[q] * f);
+      for (int q = 0; q < 4; ++q) u[q] = st ? d.u(u[q], b[k][q]) : d.s * u[q];
     }
-    if (straight.hi) put(straight, r0 + r, c0 + c, ld_s, v);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) u[q] = (float)((double)u[q] * f);
+    if (straight.hi) put(straight, r0 + r, c0 + c, ld_s, u);
     if (turned.hi) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) tile[r][c + q] = v[q];
+      for (int q = 0; q < 4; ++q) tile[r][c + q] = u[q];
     }
   }
   if (!turned.hi) return;
