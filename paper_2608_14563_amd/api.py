@@ -32,6 +32,9 @@ def dtype_code(t: torch.dtype) -> int:
     raise TypeError(f"unsupported dtype {t}")
 
 
+_Tensor = torch.Tensor
+
+
 def _p(t: Optional[torch.Tensor], dtype: Optional[torch.dtype] = None, shape=None, dev=None,
        name: str = "tensor") -> Optional[int]:
     """Device pointer of t after the checks the C ABI cannot make from a bare
@@ -41,9 +44,9 @@ def _p(t: Optional[torch.Tensor], dtype: Optional[torch.dtype] = None, shape=Non
         return None
     # the usual case on the fewest attribute reads (a step passes some thirty
     # tensors; at the smallest sizes the host's share of a call is most of it)
-    if (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype == dtype)
+    if (isinstance(t, _Tensor) and t.is_cuda and t.is_contiguous() and (t.dtype is dtype or dtype is None)
             and (dev is None or t.device == dev)
-            and (shape is None or (t.shape == shape if isinstance(shape, tuple) else t.numel() >= shape))):
+            and (t.shape == shape or shape is None or (isinstance(shape, int) and t.numel() >= shape))):
         return t.data_ptr()
     if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
         raise ValueError(f"{name}: libfpo takes GPU tensors")
@@ -78,11 +81,13 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 
 def _call(dev: torch.device, f, *args) -> None:
     """f(*args) with dev as the current device: stream handle 0 names the current device's."""
-    if dev.type != "cuda" or _current_device() == dev.index:
-        L.check(f(*args))
+    if _current_device() == dev.index:
+        status = f(*args)
     else:
         with torch.cuda.device(dev):
-            L.check(f(*args))
+            status = f(*args)
+    if status:
+        L.check(status)
 
 
 class _Keep:
