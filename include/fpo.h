@@ -452,8 +452,10 @@ int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* ro
  *   upd         W_master, state1 (momentum; may be NULL, the array or an entry, if
  *               momentum is 0), W_lp (dtype desc->ns.dtype), clip_scale as in
  *               fpo_update_bufs; W_sumsq may be NULL if clip_frac <= 0, else (and
- *               whenever given) in ||W||_F^2, out ||W'||_F^2; state2 is ignored. No
- *               buffer may be given for two matrices
+ *               whenever given) in ||W||_F^2, out ||W'||_F^2; state2 is ignored
+ * W_master, state1 and W_lp of a matrix may share memory with no other matrix buffer of the
+ * call (FPO_ERR_ARG), but that W_lp of an FPO_F32 call may be the matrix's own W_master;
+ * one gradient may be given for several matrices.
  * ns.dtype sets the precision of the products and the type of W_lp; everything else
  * is float32.
  * Returns FPO_OK or an fpo_status. */

@@ -3,6 +3,7 @@
 // memory is allocated here and nothing synchronises with the host.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -538,6 +539,34 @@ int check_distinct(const void* const* p, int64_t n, const char* who, const char*
   return FPO_OK;
 }
 
+// The memory of one buffer of a call.
+struct Span {
+  uintptr_t at, end;
+  bool out;          // written by the call
+  const char* name;
+  int mat;           // its matrix, or -1
+};
+inline Span span(const void* p, int64_t bytes, bool out, const char* name, int mat = -1) {
+  return Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, out, name, mat};
+}
+
+// No written buffer may share memory with another buffer of the call (read ones may with each
+// other). Sorts s.
+int check_spans(Span* s, int n, const char* who) {
+  std::sort(s, s + n, [](const Span& a, const Span& b) { return a.at < b.at; });
+  const Span *any = nullptr, *out = nullptr;  // those that reach furthest so far
+  for (int i = 0; i < n; ++i) {
+    const Span* hit = s[i].out && any && s[i].at < any->end ? any : out && s[i].at < out->end ? out : nullptr;
+    if (hit && hit->mat >= 0)
+      return fail(FPO_ERR_ARG, "%s: %s of matrix %d and %s of matrix %d share memory", who, hit->name, hit->mat, s[i].name,
+                  s[i].mat);
+    if (hit) return fail(FPO_ERR_ARG, "%s: %s and %s share memory", who, hit->name, s[i].name);
+    if (!any || s[i].end > any->end) any = &s[i];
+    if (s[i].out && (!out || s[i].end > out->end)) out = &s[i];
+  }
+  return FPO_OK;
+}
+
 int check_muon(const fpo_muon* o) {
   if (!o) return fail(FPO_ERR_NULL, "fpo_muon_update: opt is NULL");
   if (!(o->lr >= 0.0) || !std::isfinite(o->lr)) return fail(FPO_ERR_ARG, "fpo_muon_update: lr must be finite and >= 0");
@@ -982,6 +1011,19 @@ int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, co
   if (upd->state1)
     if (int e = check_distinct((const void* const*)upd->state1, n_mats, "fpo_muon_update", "state1")) return e;
   if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_muon_update")) return e;
+  // The momentum pass writes what the conversion reads again, and a batch its results before the
+  // next one's gradients are read. (A float32 master may be its own copy: both get the same value.)
+  Span spans[4 * fpo::kMaxMats];
+  int ns = 0;
+  for (int64_t m = 0; m < n_mats; ++m) {
+    const int64_t bytes = 4 * rows[m] * cols[m];
+    const void* lp = upd->W_lp ? upd->W_lp[m] : nullptr;
+    spans[ns++] = span(grad[m], bytes, false, "grad", (int)m);
+    spans[ns++] = span(upd->W_master[m], bytes, true, "W_master", (int)m);
+    if (upd->state1 && upd->state1[m]) spans[ns++] = span(upd->state1[m], bytes, true, "state1", (int)m);
+    if (lp && (bf16 || lp != upd->W_master[m])) spans[ns++] = span(lp, bf16 ? bytes / 2 : bytes, true, "W_lp", (int)m);
+  }
+  if (int e = check_spans(spans, ns, "fpo_muon_update")) return e;
   fpo::NsLaunch L{};
   L.steps = opt->ns.steps;
   L.coef = opt->ns.coef;
