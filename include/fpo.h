@@ -479,9 +479,10 @@ int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, co
  * others have RMSNorm:
  *   mu = mean x_t;  sigma = sqrt(mean (x_t - mu)^2 + eps)
  *   y_t = gain (x_t - mu) / sigma + bias
- *   x, y        [T, d] (dtype); y must not alias x
+ *   x, y        [T, d] (dtype)
  *   gain, bias  [d] (dtype), each nullable: ones, zeros
  *   mean, rstd  float [T] out, nullable: mu and 1 / sigma
+ * No output may share memory with an input or another output (FPO_ERR_ARG).
  * T <= 2^23, d a multiple of 8, d <= 2^22. The statistics are float32: entries up to
  * about 1e18 / sqrt(d) from the mean, whose squares can still be added.
  * Returns FPO_OK or an fpo_status. */

@@ -1062,7 +1062,14 @@ int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, cons
   if (!x || !y) return fail(FPO_ERR_NULL, "fpo_layernorm: x and y are required");
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gain, 16) || !aligned(bias, 16))
     return fail(FPO_ERR_ARG, "fpo_layernorm: tensors must be 16-byte aligned");
-  if (y == x) return fail(FPO_ERR_ARG, "fpo_layernorm: y is x");
+  const int64_t vec = desc->d * (desc->dtype == FPO_BF16 ? 2 : 4), all = desc->T * vec;
+  Span spans[6] = {span(x, all, false, "x"), span(y, all, true, "y")};
+  int ns = 2;
+  if (gain) spans[ns++] = span(gain, vec, false, "gain");
+  if (bias) spans[ns++] = span(bias, vec, false, "bias");
+  if (mean) spans[ns++] = span(mean, 4 * desc->T, true, "mean");
+  if (rstd) spans[ns++] = span(rstd, 4 * desc->T, true, "rstd");
+  if (int e = check_spans(spans, ns, "fpo_layernorm")) return e;
   fpo::LnLaunch L{};
   L.bf16 = desc->dtype == FPO_BF16;
   L.T = desc->T;

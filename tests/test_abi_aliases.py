@@ -88,3 +88,35 @@ def test_muon_neighbours_and_repeated_gradients(dev, dtype):
     assert torch.equal(own(0), kept[:numel].view(ROWS, COLS)) and not torch.equal(own(1), kept[numel:2 * numel].view(ROWS, COLS))
     for a, b in zip(alone, (grad, W, state)):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+# --------------------------------------------------------------------- layer norm
+T, D = 16, 64
+ROWS_X, ROW = T * D * 2, D * 2  # bytes of x or y, gain or bias in bf16
+
+
+def layernorm(lib, T=T, **over):
+    """Buffers that follow each other without a gap."""
+    at = dict(x=BASE, gain=BASE + ROWS_X, bias=BASE + ROWS_X + ROW, y=BASE + ROWS_X + 2 * ROW)
+    at["mean"] = at["y"] + ROWS_X
+    at["rstd"] = at["mean"] + 4 * T
+    at.update(over)
+    desc = L.LnDesc(T, D, L.FPO_BF16, L.FPO_F32, 1e-5, 0.0)
+    status = lib.fpo_layernorm(C.byref(desc), *[at[k] for k in ("x", "gain", "bias", "y", "mean", "rstd")], None)
+    return status, lib.fpo_last_error().decode()
+
+
+Y = BASE + ROWS_X + 2 * ROW
+
+
+@pytest.mark.parametrize("name,address", [
+    ("y", BASE + ROWS_X), ("y", BASE + ROWS_X + ROW), ("y", BASE + 16), ("y", BASE - ROWS_X + 16), ("mean", BASE),
+    ("mean", BASE + ROWS_X - 4), ("mean", BASE + ROWS_X), ("rstd", BASE + ROWS_X + ROW), ("rstd", Y),
+    ("rstd", Y + ROWS_X + 4), ("mean", Y + ROWS_X + 4 * T), ("gain", Y), ("bias", Y + ROWS_X - 16)])
+def test_layernorm_refuses_shared_buffers(lib, name, address):
+    status, message = layernorm(lib, **{name: address})
+    assert status == L.FPO_ERR_ARG and "share memory" in message and name in message
+
+
+def test_layernorm_of_one_row_refuses_its_gain_as_result(lib):
+    assert layernorm(lib, T=1, y=BASE + ROWS_X)[0] == L.FPO_ERR_ARG
