@@ -964,6 +964,13 @@ int fpo_orthogonalize(const fpo_ns_desc* desc, int64_t n_mats, const int64_t* ro
         return fail(FPO_ERR_ARG, "fpo_orthogonalize: O of matrix %lld is M of matrix %lld", (long long)i, (long long)j);
   const bool bf16 = desc->dtype == FPO_BF16;
   if (int e = check_ws(ws, ws_bytes, ns_ws(bf16, n_mats, rows, cols), "fpo_orthogonalize")) return e;
+  Span spans[2 * fpo::kMaxMats];
+  for (int64_t m = 0; m < n_mats; ++m) {
+    const int64_t bytes = (bf16 ? 2 : 4) * rows[m] * cols[m];
+    spans[2 * m] = span(M[m], bytes, false, "M", (int)m);
+    spans[2 * m + 1] = span(O[m], bytes, true, "O", (int)m);
+  }
+  if (int e = check_spans(spans, 2 * (int)n_mats, "fpo_orthogonalize")) return e;
   fpo::NsLaunch L{};
   L.steps = desc->steps;
   L.coef = desc->coef;
@@ -1109,6 +1116,15 @@ int fpo_layernorm_vjp(const fpo_ln_desc* desc, const void* x, const void* gain, 
   }
   if (dgain || dbias)
     if (int e = check_ws(ws, ws_bytes, ln_vjp_ws(*desc), "fpo_layernorm_vjp")) return e;
+  const int64_t n = desc->T * desc->d, esz = desc->dtype == FPO_BF16 ? 2 : 4;
+  Span spans[7] = {span(x, n * esz, false, "x"), span(dy, n * (desc->dy_dtype == FPO_BF16 ? 2 : 4), false, "dy")};
+  int ns = 2;
+  if (gain) spans[ns++] = span(gain, desc->d * esz, false, "gain");
+  if (dx) spans[ns++] = span(dx, 4 * n, true, "dx");
+  if (dx_lp) spans[ns++] = span(dx_lp, n * esz, true, "dx_lp");
+  if (dgain) spans[ns++] = span(dgain, 4 * desc->d, true, "dgain");
+  if (dbias) spans[ns++] = span(dbias, 4 * desc->d, true, "dbias");
+  if (int e = check_spans(spans, ns, "fpo_layernorm_vjp")) return e;
   fpo::LnLaunch L{};
   L.bf16 = desc->dtype == FPO_BF16;
   L.dy_bf16 = desc->dy_dtype == FPO_BF16;

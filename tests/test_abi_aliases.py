@@ -120,3 +120,39 @@ def test_layernorm_refuses_shared_buffers(lib, name, address):
 
 def test_layernorm_of_one_row_refuses_its_gain_as_result(lib):
     assert layernorm(lib, T=1, y=BASE + ROWS_X)[0] == L.FPO_ERR_ARG
+
+
+# --------------------------------------------------------------------- ranges that overlap in part
+VX, VDY, VDX, VLP = BASE, BASE + ROWS_X, BASE + 3 * ROWS_X, BASE + 5 * ROWS_X
+VG, VDG = BASE + 6 * ROWS_X, BASE + 6 * ROWS_X + ROW
+VDB = VDG + 2 * ROW
+
+
+def vjp(lib, **over):
+    at = dict(x=VX, gain=VG, dy=VDY, dx=VDX, dx_lp=VLP, dgain=VDG, dbias=VDB)
+    at.update(over)
+    desc = L.LnDesc(T, D, L.FPO_BF16, L.FPO_F32, 1e-5, 0.0)
+    status = lib.fpo_layernorm_vjp(C.byref(desc), *[at[k] for k in ("x", "gain", "dy", "dx", "dx_lp", "dgain", "dbias")], WS,
+                                   1 << 30, None)
+    return status, lib.fpo_last_error().decode()
+
+
+@pytest.mark.parametrize("name,address", [
+    ("dx", VX + 16), ("dx", VX - 2 * ROWS_X + 16), ("dx_lp", VDY + ROWS_X), ("dx_lp", VDX + ROWS_X), ("dgain", VG + 16),
+    ("dgain", VDX + 256), ("dbias", VDG + 16), ("dbias", VLP + ROWS_X - 16), ("x", VDX + ROWS_X), ("dy", VLP - 16),
+    ("gain", VDB + 16)])
+def test_layernorm_vjp_refuses_partly_shared_buffers(lib, name, address):
+    status, message = vjp(lib, **{name: address})
+    assert status == L.FPO_ERR_ARG and "share memory" in message and name in message
+
+
+@pytest.mark.parametrize("dtype", [L.FPO_BF16, L.FPO_F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,O", [((0, 1), (2, 2.5)), ((0, 1), (1.5, 3)), ((0, 1), (-0.5, 3)), ((0, 0), (0.5, 3))])
+def test_orthogonalize_refuses_partly_shared_buffers(lib, M, O, dtype):
+    """Places in units of one matrix; two sizes, of which each batch is written before the
+    next one is read."""
+    size = ROWS * COLS * (2 if dtype == L.FPO_BF16 else 4)
+    at = lambda v: ptrs(*[BASE + int(k * size) for k in v])  # noqa: E731
+    d = L.NsDesc(dtype, 5, 1e-7, None)
+    status = lib.fpo_orthogonalize(C.byref(d), 2, i64(ROWS, ROWS // 2), i64(COLS, 2 * COLS), at(M), at(O), WS, 1 << 30, None)
+    assert status == L.FPO_ERR_ARG and "share memory" in lib.fpo_last_error().decode()
