@@ -17,11 +17,14 @@ import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 import torch
 
 from oracle import operators as P
+from paper_2608_14563_amd import _lib as L
 from paper_2608_14563_amd import api
+from tests._util import host64
 
 BF, F32 = torch.bfloat16, torch.float32
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2608_14563_amd", "csrc")
@@ -183,3 +186,56 @@ def test_orthogonalize(dev, name):
         own = 1.05 * (E.to(dtype).double() - E).norm().item()
         off = (O[i].double() - E).norm().item()
         assert off <= tol + own, f"{kinds[i % len(kinds)]} matrix {i}: off by {off:.3e}, allowed {tol:.3e} + {own:.3e}"
+
+
+CLIPS = {"off": dict(clip_frac=0.0), "gradient": dict(clip_frac=0.01, clip_target=L.FPO_CLIP_GRADIENT),
+         "update": dict(clip_frac=0.01, clip_target=L.FPO_CLIP_UPDATE)}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("clip", CLIPS)
+@pytest.mark.parametrize("name", ["whole tiles and quarters", "both ways", "ragged", "ragged in float32", "small, four waves"])
+def test_muon(dev, name, clip):
+    """The step against float64: the direction counts, at this learning rate a fifth of W."""
+    rows, cols, n, dtype, turned, groups, _ = CASES[name]
+    shapes = shapes_of(rows, cols, n, turned)
+    g = torch.Generator(device=dev)
+    g.manual_seed(rows + cols + 1)
+    opt = api.MuonConfig(lr=2e-2, step=3, **CLIPS[clip])
+    rand = lambda s, k: k * torch.randn(*s, generator=g, device=dev)  # noqa: E731
+    kinds = ("normal", "tokens") if dtype == BF else ("normal",)
+    grad = [matrix(s, kinds[i % len(kinds)], g, dev) for i, s in enumerate(shapes)]
+    grad = [x * (1e-2 / x.std()) for x in grad]
+    W = [rand(s, 0.02) for s in shapes]
+    buf = [rand(s, 3e-4 if clip == "gradient" else 1e-2) for s in shapes]  # (the clip makes the gradient 2e-4)
+    sumsq = lambda ts: torch.stack([t.double().square().sum() for t in ts])  # noqa: E731
+    W_sumsq, grad_sumsq = sumsq(W), sumsq(grad)
+    W_lp = [torch.full(s, float("nan"), dtype=dtype, device=dev) for s in shapes]
+    factor = torch.full((n,), float("nan"), device=dev)
+    W0, b0, g0 = ([t.clone() for t in ts] for ts in (W, buf, grad))
+    api.fpo_muon_update(opt, grad, W, buf, W_sumsq=W_sumsq, grad_sumsq=grad_sumsq if clip == "gradient" else None,
+                        W_lp=W_lp, clip_scale=factor, dtype=dtype)
+    for i in sorted({0, 1, n // 2, n - 1}):
+        w, d, b = host64(W0[i]), host64(g0[i]), host64(b0[i])
+        args = (w, d, b, opt.lr, opt.momentum, True, opt.weight_decay, "rms", opt.step, opt.clip_frac,
+                "update" if clip == "update" else "gradient")
+        u = P.muon(*args, orthogonal=np.zeros_like(w))[3]
+        E, tol = reference(torch.from_numpy(u).to(dev), groups, dtype)
+        want, b1, k, _ = P.muon(*args, orthogonal=E.cpu().numpy())
+        size = opt.lr * P.muon_scale("rms", *w.shape)
+        # the direction's error, and float32 roundings of decay, product and sum. The update clip's factor k scales
+        # the step, and with it its error, and is itself off by the step's; the gradient clip's k scales u, whose
+        # direction O has the same size at any k
+        slack = size * tol * (2 * k if clip == "update" else 1) + 4 * 2 ** -24 * (np.linalg.norm(w) + size * E.norm().item())
+        off = np.linalg.norm(host64(W[i]) - want)
+        assert off <= slack, f"matrix {i}: W off by {off:.3e}, allowed {slack:.3e}"
+        assert off <= 0.05 * np.linalg.norm(want - w)  # (what is compared is the step, not W)
+        g_scale = k if clip == "gradient" else 1.0  # (only this clip scales what enters the momentum)
+        bound = 3 * 2 ** -24 * (opt.momentum * np.abs(b) + g_scale * np.abs(d)) + 1e-30
+        assert bool((np.abs(host64(buf[i]) - b1) <= bound).all()), f"matrix {i}: momentum"
+        rel = 1e-6 + (tol / E.norm().item() if clip == "update" else 0)
+        assert abs(float(factor[i]) - k) <= rel * k and (k < 1) == (clip != "off")
+        w1 = host64(W[i])
+        assert abs(float(W_sumsq[i]) - (w1 * w1).sum()) <= 1e-12 * (w1 * w1).sum()
+    for i in range(n):
+        assert torch.equal(grad[i], g0[i]) and torch.equal(W_lp[i], W[i].to(dtype))
