@@ -52,37 +52,17 @@ __device__ __forceinline__ void unpack4(u32x2 w, float (&v)[4]) {
   for (int k = 0; k < 4; ++k) v[k] = (float)h[k];
 }
 
-// What the epilogue adds at four rows (row .. row + 3) and VEC columns of an operand, as
-// loaded. Of a symmetric operand a lane with one column loads the four entries of row
-// `col` instead, which lie together.
-template <int VEC, bool SYM>
+// What the epilogue of the 256 x 256 tiles adds at four rows (row .. row + 3) and four columns
+// of an operand, as loaded.
 struct NsBlock {
-  static constexpr int N = VEC == 4 ? 4 : SYM ? 1 : 2;
-  u32x2 w[N];
+  u32x2 w[4];
   __device__ __forceinline__ void load(const uint16_t* p, int ld, int row, int col) {
-    if constexpr (VEC == 4) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) w[r] = *reinterpret_cast<const u32x2*>(p + (int64_t)(row + r) * ld + col);
-    } else if constexpr (SYM) {
-      w[0] = *reinterpret_cast<const u32x2*>(p + (int64_t)col * ld + row);
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) w[r >> 1][r & 1] = p[(int64_t)(row + r) * ld + col];
-    }
+    for (int r = 0; r < 4; ++r) w[r] = *reinterpret_cast<const u32x2*>(p + (int64_t)(row + r) * ld + col);
   }
-  __device__ __forceinline__ void get(float (&v)[4][VEC]) const {
-    if constexpr (VEC == 4) {
+  __device__ __forceinline__ void get(float (&v)[4][4]) const {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) unpack4(w[r], v[r]);
-    } else if constexpr (SYM) {
-      float t[4];
-      unpack4(w[0], t);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r][0] = t[r];
-    } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r][0] = f16_to_f32((uint16_t)w[r >> 1][r & 1]);
-    }
+    for (int r = 0; r < 4; ++r) unpack4(w[r], v[r]);
   }
 };
 
@@ -162,7 +142,7 @@ __global__ __launch_bounds__(256, 1) void ns_gemm_kernel(NsGemmArgs g) {
   // ---- what the epilogue adds: x of A (its low half xl for pairs), y of B
   constexpr bool HAS_X = WHAT == kPoly || (WHAT == kMul && !PAIR), HAS_XL = WHAT == kPoly && PAIR;
   constexpr bool HAS_Y = !PAIR && (WHAT == kMul || WHAT == kApplyX);
-  NsBlock<VEC, SYM> x[2][FN][4], xl[2][FN][4], y[2][FN][4];  // 256
+  NsBlock x[2][FN][4], xl[2][FN][4], y[2][FN][4];  // 256
   auto inside = [&](int row, int col) { return FAST || (row < g.M && col < g.N); };  // (blocks are in or out)
   // pairs leave the 256 x 256 core no registers to load ahead of the K loop, products of
   // two operands' entries half of them
