@@ -554,24 +554,21 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsEw a, NsPtrs p, NsMat
   }
 }
 
-// Four consecutive entries (r, c..c+3) of the result in the caller's orientation, from X
-// (n x m) or, for a tall matrix, X^T: tile by tile through LDS.
+// Four consecutive entries of X.
 template <bool PAIR>
-struct XTile {
-  float (*tile)[kNsEdge + 1];
-  __device__ __forceinline__ f32x4 load(const uint16_t* hi, const uint16_t* lo, int64_t at) const {
-    const f16x4 h = *reinterpret_cast<const f16x4*>(hi + at);
-    f32x4 v = {(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
-    if constexpr (PAIR) {
-      const f16x4 l = *reinterpret_cast<const f16x4*>(lo + at);
+__device__ __forceinline__ f32x4 load_x4(const uint16_t* hi, const uint16_t* lo, int64_t at) {
+  const f16x4 h = *reinterpret_cast<const f16x4*>(hi + at);
+  f32x4 v = {(float)h[0], (float)h[1], (float)h[2], (float)h[3]};
+  if constexpr (PAIR) {
+    const f16x4 l = *reinterpret_cast<const f16x4*>(lo + at);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] += (float)l[k];
-    }
-    return v;
+    for (int k = 0; k < 4; ++k) v[k] += (float)l[k];
   }
-};
+  return v;
+}
 
-// One 64 x 64 tile of the caller's matrix (finish4), and its share of a sum.
+// One 64 x 64 tile of the caller's matrix (finish4), by way of LDS where that is tall, and its
+// share of a sum.
 template <typename T, int WHAT, bool PAIR>
 __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p, NsMat X) {
   __shared__ float tile[kNsEdge][kNsEdge + 1];
@@ -583,12 +580,11 @@ __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p,
   const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;
   const uint16_t* hi = X.hi + mat * X.stride;
   const uint16_t* lo = hi + X.lo_off;
-  const XTile<PAIR> xt{tile};
   if (tall) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int i = k * 16 + (t >> 4), j = 4 * (t & 15);
-      const f32x4 v = xt.load(hi, lo, (int64_t)(i0 + i) * a.mp + j0 + j);
+      const f32x4 v = load_x4<PAIR>(hi, lo, (int64_t)(i0 + i) * a.mp + j0 + j);
 #pragma unroll
       for (int q = 0; q < 4; ++q) tile[j + q][i] = v[q];
     }
@@ -609,7 +605,7 @@ __global__ __launch_bounds__(256) void ns_finish_kernel(NsFinish a, NsOutPtrs p,
     if (tall)
       v = f32x4{tile[r][c], tile[r][c + 1], tile[r][c + 2], tile[r][c + 3]};
     else
-      v = xt.load(hi, lo, (int64_t)(i0 + r) * a.mp + j0 + c);
+      v = load_x4<PAIR>(hi, lo, (int64_t)(i0 + r) * a.mp + j0 + c);
     v *= a.pow2;
     const int64_t at = (int64_t)(r0 + r) * C + c0 + c;
     finish4<T, WHAT>(a, p, mat, step, k_clip, at, v, sum);
