@@ -805,7 +805,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
   };
   const auto launch = [&](auto what, const char* name, const NsGemmArgs& g, int sets) {
     constexpr int kWhat = decltype(what)::value;
-    return small ? launch_small_product(kWhat, name, g, sets, PAIR, NsMat{}, NsMat{}, false, nullptr, st)
+    return small ? launch_small_product(kWhat, name, g, PAIR, NsMat{}, NsMat{}, false, nullptr, st)
                  : launch_product<kWhat, PAIR>(name, g, sets, st);
   };
   constexpr std::integral_constant<int, kGram> gram;
@@ -858,7 +858,7 @@ hipError_t run_ns(const NsLaunch& a, const NsBatch& b) {
       // the last one finishes the caller's matrices, unless the clip needs the whole step's norm first
       const bool end = gi + 1 == pl.ngroups, fused = end && !a.clip_update;
       const NsLast last{f, o, a.muon ? kApply : kWriteO};
-      err = launch_small_product(kApplyX, fused && a.muon ? "muon_apply" : "ns_apply", g, 1, PAIR, X, end ? NsMat{} : YT,
+      err = launch_small_product(kApplyX, fused && a.muon ? "muon_apply" : "ns_apply", g, PAIR, X, end ? NsMat{} : YT,
                                  end, fused ? &last : nullptr, st);
     } else {
       err = launch_product<kApplyX, PAIR>("ns_apply", g, 1, st);

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
   constexpr int E = 8 / NW, H = NW / 2;           // chunks of eight entries a thread stores; partial sums in LDS
   __shared__ __align__(16) float red[H][kSmallEdge][kRedLd];
   const int ntm = g.M / kSmallEdge;
-  const int loc = blockIdx.x, mat = blockIdx.y, set = blockIdx.z;
+  const int loc = blockIdx.x, mat = blockIdx.y;
   int tm, tn;
   if constexpr (SYM) {
     tri_tile(loc, ntm, tm, tn);
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
     tm = loc - tn * ntm;
   }
   const int m0 = tm * kSmallEdge, n0 = tn * kSmallEdge;
-  const NsMat a = set ? g.a[1] : g.a[0], b = set ? g.b[1] : g.b[0], c = set ? g.c[1] : g.c[0];
+  const NsMat a = g.a[0], b = g.b[0], c = g.c[0];
   const int w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l = threadIdx.x & 63;
   const uint16_t* ah = a.hi + mat * a.stride;
   const uint16_t* bh = b.hi + mat * b.stride;
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
   if (w < H) each([](f32x4 v, f32x4& m) { m += v; });
   __syncthreads();
   // ---- epilogue
-  const float alpha = set ? g.alpha[1] : g.alpha[0];
+  const float alpha = g.alpha[0];
   uint16_t* ch = LAST ? nullptr : c.hi + mat * c.stride;
   uint16_t h[E][8], lo[E][8];
   float fin[LAST ? E : 1][8];
@@ -265,9 +265,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void ns_small_kernel(NsGe
 }
 
 template <int WHAT, class Last>
-void launch_small(const char* name, const NsGemmArgs& g, int sets, bool pair, const NsMat& x_of_b,
-                  const NsMat& to_t, int rows, const Last& last, hipStream_t st) {
-  const dim3 grid((unsigned)g.tiles, (unsigned)g.count, (unsigned)sets);
+void launch_small(const char* name, const NsGemmArgs& g, bool pair, const NsMat& x_of_b, const NsMat& to_t, int rows,
+                  const Last& last, hipStream_t st) {
+  const dim3 grid((unsigned)g.tiles, (unsigned)g.count);
   auto waves = [&](auto nw) {
     constexpr int NW = decltype(nw)::value;
     if (pair)
@@ -279,23 +279,23 @@ void launch_small(const char* name, const NsGemmArgs& g, int sets, bool pair, co
                  (ns_small_kernel<WHAT, false, NW, Last><<<grid, dim3(64 * NW), 0, st>>>(
                      g, x_of_b, to_t, rows, last)));
   };
-  if ((int64_t)g.tiles * g.count * sets <= kCus) waves(std::integral_constant<int, 8>{});
+  if ((int64_t)g.tiles * g.count <= kCus) waves(std::integral_constant<int, 8>{});
   else waves(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
 
-hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
+hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, bool pair, const NsMat& x_of_b,
                                 const NsMat& to_t, bool rows, const NsLast* last, hipStream_t st) {
   g.tiles = (int)ns_tiles(g.M, g.N, kSmallEdge, what != kApplyX);
   const NsNotLast no;
   switch (what) {
-    case kGram: launch_small<kGram>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
-    case kMul: launch_small<kMul>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
-    case kPoly: launch_small<kPoly>(name, g, sets, pair, x_of_b, to_t, 0, no, st); break;
+    case kGram: launch_small<kGram>(name, g, pair, x_of_b, to_t, 0, no, st); break;
+    case kMul: launch_small<kMul>(name, g, pair, x_of_b, to_t, 0, no, st); break;
+    case kPoly: launch_small<kPoly>(name, g, pair, x_of_b, to_t, 0, no, st); break;
     default:
-      if (last) launch_small<kApplyX>(name, g, sets, pair, x_of_b, to_t, 0, *last, st);
-      else launch_small<kApplyX>(name, g, sets, pair, x_of_b, to_t, rows, no, st);
+      if (last) launch_small<kApplyX>(name, g, pair, x_of_b, to_t, 0, *last, st);
+      else launch_small<kApplyX>(name, g, pair, x_of_b, to_t, rows, no, st);
       break;
   }
   return hipGetLastError();

@@ -125,13 +125,14 @@ __device__ __forceinline__ int64_t small_chunk(int row, int col, int cols) {
 // The products of small matrices: 64 x 64 tiles. B is given transposed: a symmetric one is
 // its own transpose, for kApplyX it is X^T, and x_of_b X itself. kApplyX stores C^T in to_t
 // if that has hi; with `rows` it stores C row by row, with `last` it does not store it but
-// finishes the caller's matrices (kWriteO or kApply).
+// finishes the caller's matrices (kWriteO or kApply). One set of operands: ns_choose gives small
+// matrices at most two steps a group, and only a third one's products make two.
 struct NsLast {
   NsFinish f;
   NsOutPtrs p;
   int what;
 };
-hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, int sets, bool pair, const NsMat& x_of_b,
+hipError_t launch_small_product(int what, const char* name, NsGemmArgs g, bool pair, const NsMat& x_of_b,
                                 const NsMat& to_t, bool rows, const NsLast* last, hipStream_t st);
 
 }  // namespace fpo
