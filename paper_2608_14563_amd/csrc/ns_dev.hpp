@@ -31,7 +31,7 @@ struct NsGemmArgs {
 };
 
 // What a launch computes. kGram: X X^T, B K-contiguous ([N][K] rows); the others have B
-// N-contiguous ([K][N]). kGram, kMul and kPoly: symmetric, tiles with tn <= tm. kApply: Q X.
+// N-contiguous ([K][N]). kGram, kMul and kPoly: symmetric, tiles with tn <= tm. kApplyX: Q X.
 enum { kGram = 0, kMul = 1, kPoly = 2, kApplyX = 3 };
 
 __device__ __forceinline__ uint16_t to_f16(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
