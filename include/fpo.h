@@ -505,7 +505,10 @@ int fpo_layernorm(const fpo_ln_desc* desc, const void* x, const void* gain, cons
  *   dx_t = (v - mean v - x^ mean(v x^)) / sigma~
  *   dgain = sum_t dy_t (x_t - mu) / sigma,  dbias = sum_t dy_t
  *   x            [T, d] (dtype);  gain [d] (dtype), nullable: ones
- *   dy           [T, d] (dy_dtype): e.g. fpo_output_error's g_pre
+ *   dy           [T, d] (dy_dtype): the gradient of what follows the norm. For a final norm
+ *                without bias that is fpo_output_error's g_pre, if its h_final are the centred
+ *                hidden states x_t - mu_t: their RMSNorm is the layer norm. (The logits of a
+ *                final norm with a bias are not what fpo_output_error computes.)
  *   dx           float [T, d] out, nullable;  dx_lp [T, d] (dtype) out, nullable: dx rounded once
  *   dgain, dbias float [d] out, each nullable; sums in a fixed order
  * At least one output is required; none may overlap an input or another output.
