@@ -50,9 +50,9 @@ CASES = {
 SRC = """
 #include "ns.hpp"
 using namespace fpo;
-extern "C" int choose(long n, long m, int count, int bf16, int* groups) {  // small; steps of each group, 0
-  const NsChoice c = ns_choose(n, m, count, bf16 != 0);
-  const NsPlan p = ns_plan(5, nullptr, c.first);
+extern "C" int choose(long n, long m, int count, int bf16, int steps, const double* coef, int* groups) {
+  const NsChoice c = ns_choose(n, m, count, bf16 != 0);  // (groups: steps of each, then 0)
+  const NsPlan p = ns_plan(steps, coef, c.first);
   for (int i = 0; i < p.ngroups; ++i) groups[i] = p.groups[i].count;
   groups[p.ngroups] = 0;
   return c.small;
@@ -78,18 +78,24 @@ def host(tmp_path_factory):
     lib.big_tiles.restype = lib.small_tiles.restype = C.c_long
     lib.big_tiles.argtypes = [C.c_long] * 4 + [C.c_int, C.POINTER(C.c_long)]
     lib.small_tiles.argtypes = [C.c_long, C.c_long, C.c_int]
-    lib.choose.argtypes = [C.c_long, C.c_long, C.c_int, C.c_int, C.POINTER(C.c_int)]
+    lib.choose.argtypes = [C.c_long, C.c_long, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int)]
     lib.batch_limit.argtypes = [C.c_long]
     return lib
+
+
+def groups_of(host, short, longer, n, bf16, per_step=(P.MUON_COEF,) * 5):
+    """(small tiles, steps in each group)"""
+    g = (C.c_int * 64)()
+    flat = [v for k in per_step for v in k]
+    small = host.choose(short, longer, n, bf16, len(per_step), (C.c_double * len(flat))(*flat), g)
+    return small, tuple(g[:list(g).index(0)])
 
 
 def path(host, rows, cols, n, dtype):
     """(steps of the groups, tiles of the launches) of n matrices, as CASES states them."""
     short, longer, bf16 = min(rows, cols), max(rows, cols), dtype == BF
     assert n <= host.batch_limit(short)  # one batch
-    g = (C.c_int * 64)()
-    small = host.choose(short, longer, n, bf16, g)
-    groups = tuple(g[:list(g).index(0)])
+    small, groups = groups_of(host, short, longer, n, bf16)
     np_, mp = (-(-v // 64) * 64 for v in (short, longer))
     launches = ((np_, np_, mp, 1, 1), (np_, np_, np_, 1, 1), (np_, np_, np_, 2, 1), (np_, mp, np_, 1, 0))
     out = []
@@ -111,13 +117,13 @@ def test_paths(host, name):
 
 def test_small_tiles_take_one_set_of_operands(host):
     """Their groups have two steps at most: no launch multiplies two sets of operands."""
-    g = (C.c_int * 64)()
     for n in range(8, 1025, 56):
         for m in range(n, 4 * n + 1, 56):
             for count in (1, 2, 5, 9, 20, 64):
                 for bf16 in (0, 1):
-                    if count <= host.batch_limit(n) and host.choose(n, m, count, bf16, g):
-                        assert max(g[:list(g).index(0)]) <= 2
+                    small, groups = groups_of(host, n, m, count, bf16)
+                    if small:
+                        assert max(groups) <= 2
 
 
 # --------------------------------------------------------------------- float64 on the GPU
@@ -125,17 +131,18 @@ def to_fp16(x):
     return (x * 512).half().double() / 512
 
 
-def iterate(M, groups, store=lambda x: x):
-    """Five steps in float64, in the given groups, `store` applied to every matrix kept."""
+def iterate(M, groups, store=lambda x: x, per_step=(P.MUON_COEF,) * 5):
+    """The steps in float64, in the given groups, `store` applied to every matrix kept."""
     X = M.double()
     X = X if X.shape[0] <= X.shape[1] else X.t().contiguous()
     X = X / (X.square().sum().sqrt() + 1e-7)
-    a, b, c = P.MUON_COEF
-    eye = torch.eye(X.shape[0], dtype=torch.float64, device=X.device)
+    eye, at = torch.eye(X.shape[0], dtype=torch.float64, device=X.device), 0
     for count in groups:
         X = store(X)
         A, Q = store(X @ X.t()), None
         for j in range(count):
+            a, b, c = per_step[at]
+            at += 1
             B = store(a * eye + b * A + c * (A @ A))
             Q = B if Q is None else store(B @ Q)
             if j + 1 < count:
@@ -144,12 +151,12 @@ def iterate(M, groups, store=lambda x: x):
     return X if M.shape[0] <= M.shape[1] else X.t()
 
 
-def reference(M, groups, dtype):
+def reference(M, groups, dtype, per_step=(P.MUON_COEF,) * 5):
     """(float64 result, tolerance of the unrounded direction)."""
-    E = iterate(M, (1,) * 5)
+    E = iterate(M, (1,) * len(per_step), per_step=per_step)
     if dtype == F32:
         return E, 16 * (3 * max(M.shape)) ** 0.5 * 2 ** -24 * E.norm().item()
-    return E, 2 * (iterate(M, groups, to_fp16) - E).norm().item()
+    return E, 2 * (iterate(M, groups, to_fp16, per_step) - E).norm().item()
 
 
 def matrix(shape, kind, g, dev):
@@ -186,6 +193,37 @@ def test_orthogonalize(dev, name):
         own = 1.05 * (E.to(dtype).double() - E).norm().item()
         off = (O[i].double() - E).norm().item()
         assert off <= tol + own, f"{kinds[i % len(kinds)]} matrix {i}: off by {off:.3e}, allowed {tol:.3e} + {own:.3e}"
+
+
+
+# case, coefficients of each step: steps in each group
+D, CUBIC, VARIED = P.MUON_COEF, (1.5, -0.5, 0.0), ((4.0, -7.0, 4.0), P.MUON_COEF, (1.875, -1.25, 0.375))
+STEPS = [("128 tiles", (D,), (1,)), ("128 tiles", (D,) * 3, (3,)), ("128 tiles", (D,) * 4, (3, 1)),
+         ("128 tiles", (D,) * 6, (3, 2, 1)), ("128 tiles", (CUBIC,) * 12, (3, 2, 1, 2, 1, 2, 1)), ("128 tiles", VARIED, (2, 1)),
+         ("small, two a group", (D,) * 2, (2,)), ("small, two a group", (D,) * 4, (2, 1, 1)),
+         ("small, two a group", (D,) * 6, (2, 1, 2, 1)), ("small, two a group", VARIED, (2, 1))]
+
+
+@pytest.mark.parametrize("name,per_step,groups", STEPS)
+def test_groups(host, name, per_step, groups):
+    rows, cols, n = CASES[name][:3]
+    assert groups_of(host, min(rows, cols), max(rows, cols), n, 1, per_step)[1] == groups
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,per_step,groups", STEPS)
+def test_steps_and_coefficients(dev, name, per_step, groups):
+    rows, cols, n, dtype, turned = CASES[name][:5]
+    g = torch.Generator(device=dev)
+    g.manual_seed(rows + len(per_step))
+    M = [matrix(s, "normal", g, dev).to(dtype) for s in shapes_of(rows, cols, n, turned)]
+    O = [torch.full_like(m, float("nan")) for m in M]
+    api.fpo_orthogonalize(M, O, steps=len(per_step), coefs=per_step)
+    for i in (0, n - 1):
+        E, tol = reference(M[i], groups, dtype, per_step)
+        own = 1.05 * (E.to(dtype).double() - E).norm().item()
+        off = (O[i].double() - E).norm().item()
+        assert off <= tol + own, f"matrix {i}: off by {off:.3e}, allowed {tol:.3e} + {own:.3e}"
 
 
 CLIPS = {"off": dict(clip_frac=0.0), "gradient": dict(clip_frac=0.01, clip_target=L.FPO_CLIP_GRADIENT),
