@@ -407,15 +407,20 @@ int fpo_cosine(int64_t n_pairs, const int64_t* numel, const float* const* A,
  *   rows, cols  [host] int64 [n_mats], multiples of 8; rows * cols, each
  *               rounded up to 64, at most 2^29 (FPO_F32: 2^28)
  *   M           [host] n_mats pointers to [rows, cols] (dtype), read only
- *   O           [host] n_mats pointers to [rows, cols] (dtype), out; no buffer twice,
- *               and none that overlaps a matrix of M
+ *   O           [host] n_mats pointers to [rows, cols] (dtype), out; none may share
+ *               memory with another one or a matrix of M (FPO_ERR_ARG)
  * dtype FPO_BF16: bf16 in and out; products of fp16 operands (scaled by powers of
  * two, more digits than bf16), fp32 accumulation. FPO_F32: float32 in and out,
  * products to about fp32 precision (pairs of fp16, three products).
  * A matrix of zeros gives zeros (with eps 0 too). Non-finite entries give a matrix
  * of unspecified values; the other matrices of the call are not affected. Singular
- * values below about 4e-5 of the norm (the size of what rounding a matrix to bf16 adds;
- * fp32: 1e-7) carry rounding noise, enlarged as they are (3.4445 times a step).
+ * values below about 4e-5 of ||M||_F + eps (the size of what rounding a matrix to bf16
+ * adds; fp32: 1e-7) carry rounding noise, enlarged as they are (3.4445 times a step).
+ * Workspace: with n <= m the sides, about 2 n m + 5 n^2 (matrices of a few hundred rows:
+ * 4 n m + 5 n^2) entries of 2 bytes (FPO_F32: 4) a matrix, for the matrices of equal
+ * sides that are computed at once: with t = n / 256, at most the larger of 4 and
+ * 4096 / (t (t + 1)), and 64. Nine 4096 x 12288 take 3.4 GB, sixteen or more 6.0 GB (FPO_F32:
+ * 12.0 GB); calls of fewer matrices take less.
  * coef  [host] 3 * steps doubles (a, b, c of each step), NULL: the defaults. They are
  *       refused (FPO_ERR_ARG) if they let a singular value in [0, 1] grow past 1024
  *       in any step.
@@ -484,7 +489,8 @@ int fpo_muon_update(const fpo_muon* opt, int64_t n_mats, const int64_t* rows, co
  *   mean, rstd  float [T] out, nullable: mu and 1 / sigma
  * No output may share memory with an input or another output (FPO_ERR_ARG).
  * T <= 2^23, d a multiple of 8, d <= 2^22. The statistics are float32: entries up to
- * about 1e18 / sqrt(d) from the mean, whose squares can still be added.
+ * about 1e18 / sqrt(d) from the mean, whose squares can still be added, and with an eps
+ * under 1e-30 (0 too) rows whose deviation is 1e-15 at least.
  * Returns FPO_OK or an fpo_status. */
 typedef struct {
   int64_t T, d;

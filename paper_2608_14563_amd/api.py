@@ -1,5 +1,6 @@
-"""Python binding of libfpo: the calls of include/fpo.h under the same names, taking torch tensors. Argument marshalling only: every step of the
-path runs in the HIP library; torch supplies device memory and the stream.
+"""Python binding of libfpo: the calls of include/fpo.h under the same names,
+taking torch tensors. Argument marshalling only: every step of the path runs
+in the HIP library; torch supplies device memory and the stream.
 
 All tensors must be on the same CUDA (HIP) device and contiguous. The
 operand dtype follows h_final / g_tilde_lp: torch.bfloat16 (FPO_BF16) or
@@ -398,7 +399,7 @@ def fpo_orthogonalize(M, O, steps: int = 5, coefs=None, eps: float = 1e-7, ws=No
     """O[i] = the Newton-Schulz orthogonalisation of the matrix M[i] (bfloat16 or
     float32, all the same); any shapes together. coefs: (a, b, c), or one for
     each step (default: 3.4445, -4.7750, 2.0315). The workspace does not depend
-    on the steps."""
+    on the steps. No O may share memory with another one or with an M."""
     n = len(M)
     k = _Keep()
     if n == 0 or len(O) != n:
@@ -445,7 +446,9 @@ def fpo_muon_update(opt: MuonConfig, grad, W_master, state, W_sumsq=None, grad_s
     """The Muon step on float32 masters (matrices of any shapes). state: the
     momentum buffers (None only with momentum 0). dtype: precision of the
     products and type of W_lp. W_sumsq (float64, in/out) is needed by the clip
-    (clip_frac > 0), grad_sumsq by the gradient clip only."""
+    (clip_frac > 0), grad_sumsq by the gradient clip only. Masters, states and
+    copies may not share memory with each other or with a gradient, but that a
+    float32 master may be its own copy."""
     n = len(grad)
     k = _Keep()
     if n == 0:
@@ -473,7 +476,8 @@ def fpo_muon_update(opt: MuonConfig, grad, W_master, state, W_sumsq=None, grad_s
 
 # --------------------------------------------------------------------- layer norm
 def fpo_layernorm(x, gain, bias, y, mean=None, rstd=None, eps=1e-5):
-    """Layer norm of the rows of x [T, d] into y; gain and bias [d] may be None."""
+    """Layer norm of the rows of x [T, d] into y; gain and bias [d] may be None. No
+    output may share memory with an input or another output (the VJP's neither)."""
     T, d = x.shape
     op, dev = x.dtype, x.device
     desc = L.LnDesc(T, d, dtype_code(op), L.FPO_F32, eps, 0.0)

@@ -6,7 +6,7 @@
 //   dgain = sum_t dy (x - mu) / sigma, dbias = sum_t dy
 // Both are bound by HBM: a row is read once into registers, its statistics are two
 // reductions over the lanes that share it (the squares are of differences from the
-// mean, so that a large mean costs no digits), and everything else is elementwise.
+// mean, so that a large mean costs only the digits of its own rounding), and everything else is elementwise.
 //
 // A row is shared by 16 lanes (d up to 128), 32 (256), 64 (1024 or 2048), 256 (up to 4096),
 // 512 (8192) or 1024 (16384), each holding up to four chunks of eight neighbouring elements; longer rows are
@@ -481,7 +481,9 @@ int ln_vjp_blocks(int64_t T, int64_t d) {
   const int64_t groups = ceil_div(T, ln_threads(s.lanes) / s.lanes);
   // Few rows are left to one workgroup, whose sums are the results: another turn of it takes
   // 0.8 us (64 lanes a row) to 2 us (d 8192), the second launch 2.5 us and 3 us of the host.
-  // (T 16, d 512: 9.7 -> 6.9 us, from a graph 5.4 -> 6.0; T 2, d 4096: 9.6 -> 6.8, 6.3 -> 5.9.)
+  // Eager, T 16, d 512: 9.5 -> 6.7 us; 2 x 4096: 9.5 -> 6.8; 2 x 8192: 9.4 -> 6.9. From a graph
+  // two turns gain (8 x 512: 5.3 -> 4.2 us; 2 x 4096: 6.3 -> 5.9; 2 x 8192: 7.1 -> 7.0), four lose
+  // (16 x 512: 5.4 -> 6.0; 32 x 256: 5.5 -> 5.9; 64 x 128: 6.0 -> 6.2) less than they gain eager.
   if (groups <= (s.lanes <= 64 ? 4 : s.lanes <= 512 ? 2 : 1)) return 1;
   return (int)std::min<int64_t>(groups, kCus * per_cu);
 }

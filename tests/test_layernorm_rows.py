@@ -17,7 +17,7 @@ import torch
 from paper_2608_14563_amd import _lib as L
 from paper_2608_14563_amd import api
 from tests._util import host64
-from tests.test_parity_layernorm import check, rows, vjp_tol
+from tests.test_parity_layernorm import check, forward_tol, rows, vjp_tol
 
 BF, F32 = torch.bfloat16, torch.float32
 
@@ -68,3 +68,27 @@ def test_parameter_gradients(dev, T, d, dtype, dy_dtype):
     check("dgain", out["dgain"], dg, tdg, F32)
     check("dbias", out["dbias"], db, tdb, F32)
     assert np.isfinite(host64(out["dgain"])).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 1032, 4104])
+@pytest.mark.parametrize("scale,eps", [(1e-14, 0.0), (1e-14, 1e-30), (None, 0.0), (None, 1e-5)], ids=["small", "small-eps", "large", "large-eps"])
+def test_range_of_the_statistics(dev, d, scale, eps):
+    """Deviations from 1e-15 (here ten times that, and a row of 1e-15) up to entries of 1e18 /
+    sqrt(d): of normal values none is more than 6 deviations from the mean."""
+    T = 9
+    x = rows(T, d, dev, F32, seed=d)
+    assert x.abs().max() < 6
+    x.mul_(1e18 / (6 * d ** 0.5) if scale is None else scale)
+    if scale is not None:
+        x[3] *= 0.1
+    gain, dy = rows(1, d, dev, F32, seed=1)[0], 0.02 * rows(T, d, dev, F32, seed=2)
+    y, dx, dgain = torch.empty_like(x), torch.empty_like(x), torch.empty(d, device=dev)
+    api.fpo_layernorm(x, gain, None, y, eps=eps)
+    api.fpo_layernorm_vjp(x, gain, dy, dx=dx, dgain=dgain, eps=eps)
+    want, _, _, tol = forward_tol(host64(x), host64(gain), None, eps)
+    check("y", y, want, tol, F32)
+    n, slots = layout(T, d)
+    wx, wg, _, tdx, tdg, _ = vjp_tol(host64(x), host64(gain), host64(dy), eps, 0.0, -(-T // (n * slots)) + slots)
+    check("dx", dx, wx, tdx, F32)
+    check("dgain", dgain, wg, tdg, F32)
